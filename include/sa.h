@@ -10,7 +10,10 @@
  *      (sa_sparse_prefill).
  * Beside this path: steps 1 and 2 as one call (sa_estimate_and_index), one
  * decode step over the same index (sa_sparse_decode) and the offline per-head
- * pattern search (sa_search_patterns).
+ * pattern search (sa_search_patterns); rotary positions of Q and K in front of it
+ * (sa_rotary_embed); and behind it a cache that holds K and V in 8 bits
+ * (sa_cache_append) with the decode step over the index (sa_cache_decode) and causal
+ * attention of the newest tokens (sa_cache_attend) that read it.
  *
  * Conventions
  *   - C99 types only.  Q, K, V, O are DEVICE pointers to raw bf16 (16-bit)
@@ -238,6 +241,112 @@ sa_status sa_search_scratch_bytes(const sa_ctx *ctx, size_t *bytes);
 sa_status sa_search_patterns(sa_ctx *ctx, const void *Q, const void *K, const void *V, sa_scores scores,
                              int64_t target_pairs, int64_t eps_pairs, void *scratch_dev,
                              size_t scratch_bytes, sa_search_head *out_host, void *hip_stream);
+
+/* ---- rotary positions, and the cache in 8 bits ---------------------------------------------------
+ * Calls that take a number of tokens of their own take their tensors as sa_rows: a DEVICE tensor
+ * [heads][n][128] of bf16, its 128 elements adjacent, strides in elements, 0 for both =>
+ * contiguous.  The address must be 16-byte aligned, strides positive multiples of 8; any order of heads and
+ * rows will do.  The rows of an output must not overlap one another.  These calls run on the current
+ * device, which must be the one of the stream and of every pointer, and need no workspace unless they say so. */
+typedef struct {
+  void *data;
+  int64_t head_stride, row_stride;
+} sa_rows;
+
+/* Which elements of a row make pair i of the first rotary_dim:
+ *   SA_ROTARY_HALF         i and i + rotary_dim/2
+ *   SA_ROTARY_INTERLEAVED  2i and 2i + 1 */
+typedef enum { SA_ROTARY_HALF = 0, SA_ROTARY_INTERLEAVED = 1 } sa_rotary_layout;
+
+/* Frequencies w_i (radians per position) from w = theta^(-2i / rotary_dim):
+ *   SA_SCALING_NONE        w
+ *   SA_SCALING_LINEAR      w / factor
+ *   SA_SCALING_BASE        theta * factor^(rotary_dim / (rotary_dim - 2)) in place of theta (as NONE where rotary_dim is 2)
+ *   SA_SCALING_WAVELENGTH  t w + (1 - t) w / factor, t = clamp((original_len w / 2pi - low) / (high - low), 0, 1):
+ *                          pairs that turn more than `high` times in the original length stay, those that
+ *                          turn less than `low` times are slowed by factor
+ *   SA_SCALING_RAMP        (1 - t) w + t w / factor, t = clamp((i - a) / max(b - a, 0.001), 0, 1),
+ *                          a = max(floor(d(high)), 0), b = min(ceil(d(low)), rotary_dim - 1),
+ *                          d(r) = rotary_dim ln(original_len / (2pi r)) / (2 ln theta), the pair that turns r times */
+typedef enum {
+  SA_SCALING_NONE = 0,
+  SA_SCALING_LINEAR = 1,
+  SA_SCALING_BASE = 2,
+  SA_SCALING_WAVELENGTH = 3,
+  SA_SCALING_RAMP = 4
+} sa_rotary_scaling;
+
+typedef struct {
+  int32_t rotary_dim; /* even, <= 128; 0 => 128.  The elements behind it pass unchanged */
+  int32_t layout;     /* sa_rotary_layout */
+  int32_t scaling;    /* sa_rotary_scaling */
+  int32_t transposed; /* 0 or 1; 1: angles negated, the transposed map: what turns an output's gradient into
+                       * the input's, and the inverse where amplitude is 1 */
+  double theta;       /* > 1; 0 => 10000 */
+  double factor;      /* scalings: >= 1 */
+  double low, high;   /* WAVELENGTH, RAMP: 0 < low < high */
+  double original_len;/* WAVELENGTH, RAMP: > 0 */
+  double amplitude;   /* sines and cosines are multiplied by it, > 0; 0 => 1, with RAMP 0.1 ln(factor) + 1 */
+} sa_rotary_config;
+
+typedef struct sa_rotary sa_rotary; /* opaque, host memory: frequencies; serves any context, thread and device */
+
+sa_status sa_rotary_create(const sa_rotary_config *cfg, sa_rotary **out);
+void sa_rotary_destroy(sa_rotary *rotary);
+
+/* Row t of every head of Q [n_q_heads][n] and K [n_kv_heads][n] turned to position pos + t, or to
+ * positions[t] (DEVICE int32[n]; negative ones and repeats are fine; then pos is not used):
+ *   pair (x, y) -> (x cos - y sin, x sin + y cos) * amplitude at angle position * w_i.
+ * Angles are exact to 2^-32 of a turn at any position; the arithmetic is fp32, rounded to bf16 once.
+ * Q_out may be Q with the same strides (in place), likewise K_out; other overlaps are not allowed.
+ * Q.data or K.data may be NULL: that side is left out.  0 <= pos, pos + n <= 2^31; n = 0 does nothing. */
+sa_status sa_rotary_embed(sa_ctx *ctx, const sa_rotary *rotary, sa_rows Q, sa_rows K, int64_t n, int64_t pos,
+                          const int32_t *positions, sa_rows Q_out, sa_rows K_out, void *hip_stream);
+
+/* The types of the cache's codes (OCP 8-bit floating point): e4m3 (no infinities, largest 448) and e5m2 (57344). */
+typedef enum { SA_CACHE_E4M3 = 0, SA_CACHE_E5M2 = 1 } sa_cache_type;
+
+/* A cache of K and V, DEVICE buffers owned by the caller.  Of `tokens` tokens the first
+ * tokens / block * block stand in full blocks of `block` (the context's) tokens, as codes with one scale for each
+ * block and KV head; the rest, the open block, stands in bf16.  A key is code * scale, exactly a bf16 value.
+ *   k, v              [n_kv_heads][capacity][128]      codes
+ *   k_scale, v_scale  [n_kv_heads][capacity / block]   fp32, powers of two
+ *   k_open, v_open    [n_kv_heads][block][128]         bf16, token t of the open block in row t % block
+ * k, v, k_open and v_open 16-byte aligned.  What stands behind the tokens is never read. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  void *k_open, *v_open;
+  int64_t capacity; /* tokens, a positive multiple of block, <= 2^30 */
+  int32_t type;     /* sa_cache_type */
+} sa_cache;
+
+/* Byte sizes of the six buffers, in sa_cache member order. */
+sa_status sa_cache_bytes(const sa_ctx *ctx, int64_t capacity, size_t sizes[6]);
+
+/* Append K, V [n_kv_heads][n] (rotated where the model rotates) to a cache that holds pos tokens.  A block
+ * that becomes full gets the least power of two s >= 2^-100 with (largest finite magnitude) <= s * (largest of
+ * the type), 1 if all its values are 0, and the codes nearest to value / s (ties to even): the bytes depend on
+ * the block's values alone, not on how many calls brought them.  NaN stays NaN; an infinity becomes NaN in
+ * e4m3, which has none.  pos + n <= capacity; n = 0 does nothing.  The earlier rows of the open block are read
+ * from k_open, v_open, so pos can be taken back inside the open block, but not into a full one. */
+sa_status sa_cache_append(sa_ctx *ctx, const sa_cache *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                          void *hip_stream);
+
+/* sa_sparse_decode on a cache that holds tokens 0 .. pos: same index, same kept keys, same q, o and pos, same
+ * use of ctx's workspace.  ctx's strides of K and V do not matter. */
+sa_status sa_cache_decode(sa_ctx *ctx, const sa_cache *cache, const void *q, sa_index idx, int64_t pos, void *o,
+                          void *hip_stream);
+
+/* Causal attention of the newest n tokens of a cache that holds pos + n: the query of row t of Q
+ * [n_q_heads][n] attends tokens 0 .. pos + t, with the prefill's scaled softmax.  n from 1 (a decode step without
+ * an index) over a handful of drafted tokens to chunks of a prompt; n * n_q_heads < 2^30.  O may be Q with the
+ * same strides.
+ * scratch: DEVICE, 256-byte aligned, sa_cache_attend_scratch_bytes bytes (the same for every n and pos; calls
+ * that may overlap in time need one each, as replays of captured graphs on several streams do). */
+sa_status sa_cache_attend_scratch_bytes(const sa_ctx *ctx, size_t *bytes);
+sa_status sa_cache_attend(sa_ctx *ctx, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
+                          void *scratch_dev, size_t scratch_bytes, void *hip_stream);
 
 const char *sa_last_error(const sa_ctx *ctx);
 

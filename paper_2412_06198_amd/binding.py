@@ -6,6 +6,7 @@ another implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -13,6 +14,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsa_prefill.so")
 
 SA_PATTERN_AUTO, SA_TRIANGULAR, SA_INTERVAL_SLASH, SA_BLOCK_CLUSTER = -1, 0, 1, 2
+SA_ROTARY_HALF, SA_ROTARY_INTERLEAVED = 0, 1
+SA_SCALING_NONE, SA_SCALING_LINEAR, SA_SCALING_BASE, SA_SCALING_WAVELENGTH, SA_SCALING_RAMP = 0, 1, 2, 3, 4
+SA_CACHE_E4M3, SA_CACHE_E5M2 = 0, 1
 _STATUS = {0: "SA_OK", 1: "SA_ERR_INVALID_ARG", 2: "SA_ERR_UNSUPPORTED",
            3: "SA_ERR_BUFFER_TOO_SMALL", 4: "SA_ERR_HIP"}
 
@@ -47,6 +51,21 @@ class SaIndex(C.Structure):
                 ("blkcols", C.c_void_p)]
 
 
+class SaRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class SaRotaryConfig(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("transposed", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("original_len", C.c_double), ("amplitude", C.c_double)]
+
+
+class SaCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_open", C.c_void_p), ("v_open", C.c_void_p), ("capacity", C.c_int64), ("type", C.c_int32)]
+
+
 _lib = None
 
 
@@ -79,6 +98,18 @@ def library():
         lib.sa_search_scratch_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
         lib.sa_search_patterns.argtypes = [vp, vp, vp, vp, SaScores, C.c_int64, C.c_int64, vp, C.c_size_t,
                                            C.POINTER(SaSearchHead), vp]
+        lib.sa_rotary_create.argtypes = [C.POINTER(SaRotaryConfig), C.POINTER(vp)]
+        lib.sa_rotary_destroy.argtypes = [vp]
+        lib.sa_rotary_destroy.restype = None
+        lib.sa_rotary_embed.argtypes = [vp, vp, SaRows, SaRows, C.c_int64, C.c_int64, vp, SaRows, SaRows, vp]
+        lib.sa_cache_bytes.argtypes = [vp, C.c_int64, C.POINTER(C.c_size_t)]
+        lib.sa_cache_append.argtypes = [vp, C.POINTER(SaCache), SaRows, SaRows, C.c_int64, C.c_int64, vp]
+        lib.sa_cache_decode.argtypes = [vp, C.POINTER(SaCache), vp, SaIndex, C.c_int64, vp, vp]
+        lib.sa_cache_attend_scratch_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+        lib.sa_cache_attend.argtypes = [vp, C.POINTER(SaCache), SaRows, C.c_int64, C.c_int64, SaRows, vp, C.c_size_t, vp]
+        for f in ("sa_rotary_create", "sa_rotary_embed", "sa_cache_bytes", "sa_cache_append", "sa_cache_decode",
+                  "sa_cache_attend_scratch_bytes", "sa_cache_attend"):
+            getattr(lib, f).restype = st
         for f in ("sa_default_budgets", "sa_create", "sa_scores_bytes", "sa_index_bytes",
                   "sa_workspace_bytes", "sa_set_workspace", "sa_estimate_patterns",
                   "sa_build_index", "sa_sparse_prefill", "sa_sparse_prefill_counted",
@@ -210,6 +241,110 @@ def sa_search_patterns(ctx, Q, K, V, scores: SaScores, target_pairs, eps_pairs, 
             for r in out]
 
 
+def sa_rotary_create(cfg: SaRotaryConfig):
+    rotary = C.c_void_p()
+    _check(library().sa_rotary_create(C.byref(cfg), C.byref(rotary)))
+    return rotary
+
+
+def sa_rotary_destroy(rotary):
+    library().sa_rotary_destroy(rotary)
+
+
+def sa_rotary_embed(ctx, rotary, Q: SaRows, K: SaRows, n, pos, positions, Q_out: SaRows, K_out: SaRows, stream=None):
+    """Q, K, Q_out, K_out as _rows makes them; an empty SaRows() leaves a side out."""
+    handle = rotary.handle if isinstance(rotary, Rotary) else rotary
+    _check(library().sa_rotary_embed(ctx, handle, Q, K, n, pos, _ptr(positions), Q_out, K_out, stream), ctx)
+
+
+def sa_cache_bytes(ctx, capacity):
+    out = (C.c_size_t * 6)()
+    _check(library().sa_cache_bytes(ctx, capacity, out))
+    return list(out)
+
+
+def _cache(cache):
+    return cache.struct() if isinstance(cache, Cache) else cache
+
+
+def sa_cache_append(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
+    _check(library().sa_cache_append(ctx, _cache(cache), K, V, n, pos, stream), ctx)
+
+
+def sa_cache_decode(ctx, cache, q, index: SaIndex, pos, o, stream=None):
+    _check(library().sa_cache_decode(ctx, _cache(cache), _ptr(q), index, pos, _ptr(o), stream), ctx)
+
+
+def sa_cache_attend_scratch_bytes(ctx) -> int:
+    out = C.c_size_t()
+    _check(library().sa_cache_attend_scratch_bytes(ctx, C.byref(out)), ctx)
+    return out.value
+
+
+def sa_cache_attend(ctx, cache, Q: SaRows, n, pos, O: SaRows, scratch, scratch_bytes, stream=None):
+    _check(library().sa_cache_attend(ctx, _cache(cache), Q, n, pos, O, _ptr(scratch), scratch_bytes, stream), ctx)
+
+
+class Rotary:
+    """Frequencies of a rotation; the keywords are the fields of sa_rotary_config."""
+
+    def __init__(self, **config):
+        self.handle = None
+        cfg = SaRotaryConfig()
+        for k, v in config.items():
+            if k not in _ROTARY_FIELDS:
+                raise SaError(1, f"sa_rotary_config has no field {k}")
+            setattr(cfg, k, v)
+        self.cfg = cfg
+        self.handle = sa_rotary_create(cfg)
+
+    def __del__(self):
+        try:
+            if self.handle is not None:
+                sa_rotary_destroy(self.handle)
+                self.handle = None
+        except Exception:
+            pass
+
+
+_NOTHING = contextlib.nullcontext()
+_ROTARY_FIELDS = {name for name, _ in SaRotaryConfig._fields_}
+
+
+class Cache:
+    """The six buffers of an 8-bit key/value cache (see sa_cache in include/sa.h): k, v uint8 [n_kv_heads, capacity, 128],
+    k_scale, v_scale fp32 [n_kv_heads, capacity / block], k_open, v_open bf16 [n_kv_heads, block, 128], contiguous."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_open, v_open, cache_type=SA_CACHE_E4M3):
+        heads, capacity, d = k.shape
+        block = k_open.shape[1]
+        want = [(heads, capacity, d)] * 2 + [(heads, capacity // block)] * 2 + [(heads, block, d)] * 2
+        self.tensors = (k, v, k_scale, v_scale, k_open, v_open)
+        for t, shape, size in zip(self.tensors, want, (1, 1, 4, 4, 2, 2)):
+            if tuple(t.shape) != shape or t.element_size() != size or not t.is_contiguous() or t.device != k.device:
+                raise SaError(1, f"a cache buffer is not a contiguous tensor of {shape} with {size} bytes an element on {k.device}")
+        if d != 128 or capacity % block:
+            raise SaError(1, "a cache holds rows of 128 elements and whole blocks")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_open, self.v_open = self.tensors
+        self.heads, self.capacity, self.block, self.type = heads, capacity, block, cache_type
+        self._struct = SaCache(*[t.data_ptr() for t in self.tensors], capacity, cache_type)
+
+    def struct(self):
+        return self._struct
+
+
+def _rows(t, heads, device, what):
+    """A [heads, n, 128] bf16 tensor on GPU `device` as sa_rows; its last dimension adjacent, any order of the others."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != heads or shape[2] != 128 or stride[2] != 1 or t.element_size() != 2:
+        raise SaError(1, f"{what} must be a 16-bit tensor [{heads}, n, 128] with adjacent elements")
+    if t.get_device() != device:
+        raise SaError(1, f"{what} is not on the session's device {device}")
+    if stride[0] <= 0 and stride[1] <= 0 and shape[0] * shape[1] > 1:  # two zeros would stand for contiguous rows
+        raise SaError(1, f"{what} repeats one row")
+    return SaRows(t.data_ptr(), stride[0], stride[1])
+
+
 class Session:
     """Owns a context plus the torch-allocated score / index / workspace buffers of one shape."""
 
@@ -220,6 +355,7 @@ class Session:
         self.torch = torch
         self.device = torch.device(device)
         self._known_index = None
+        self._attend_scratch = None
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
         cfg = SaConfig()
         cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim = n_q_heads, n_kv_heads, 128
@@ -308,6 +444,83 @@ class Session:
         """The same step through the entry point that keeps its partial results in the library's
         static device array (no workspace needed, nothing allocated)."""
         sa_sparse_decode_static(self.ctx, q, K, V, self._index(), pos, o, self.stream())
+
+    def _current(self, device):
+        """A context in which the session's device, which the library launches on, is the current one."""
+        return _NOTHING if self.torch.cuda.current_device() == device else self.torch.cuda.device(device)
+
+    def rotate(self, rotary, Q, K, Q_out, K_out, pos=0, positions=None):
+        """Rotary positions of Q [n_q_heads, n, 128] and K [n_kv_heads, n, 128] (either may be None), positions pos,
+        pos + 1, ... or an int32 tensor of n; the outputs may be the inputs."""
+        device = self._device_index()
+        n = (K if Q is None else Q).shape[1]
+        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        rows = []
+        for x, y, heads in ((Q, Q_out, hq), (K, K_out, hkv)):
+            if x is None:
+                rows += [SaRows(), SaRows()]
+                continue
+            if x.shape[1] != n or y.shape[1] != n:
+                raise SaError(1, "Q, K and the outputs must have the same number of rows")
+            rows += [_rows(x, heads, device, "a tensor to rotate"), _rows(y, heads, device, "an output")]
+        if positions is not None and (positions.dtype != self.torch.int32 or tuple(positions.shape) != (n,) or
+                                      not positions.is_contiguous() or positions.get_device() != device):
+            raise SaError(1, "positions must be a contiguous int32 tensor on the session's device, one per row")
+        with self._current(device):
+            sa_rotary_embed(self.ctx, rotary, rows[0], rows[2], n, pos, positions, rows[1], rows[3], self.stream())
+
+    def cache(self, capacity, cache_type=SA_CACHE_E4M3):
+        """An empty 8-bit cache for `capacity` tokens (a multiple of block)."""
+        sizes = sa_cache_bytes(self.ctx, capacity)
+        h, b, t = self.cfg.n_kv_heads, self.cfg.block, self.torch
+        kinds = [((h, capacity, 128), t.uint8)] * 2 + [((h, capacity // b), t.float32)] * 2 + [((h, b, 128), t.bfloat16)] * 2
+        bufs = [t.empty(shape, dtype=kind, device=self.device) for shape, kind in kinds]
+        assert [x.nbytes for x in bufs] == sizes
+        return Cache(*bufs, cache_type)
+
+    def _own_cache(self, cache):
+        if cache.heads != self.cfg.n_kv_heads or cache.block != self.cfg.block:
+            raise SaError(1, f"the cache has {cache.heads} heads and blocks of {cache.block}, the session {self.cfg.n_kv_heads} and {self.cfg.block}")
+        device = self._device_index()
+        if cache.k.get_device() != device:
+            raise SaError(1, f"the cache is not on the session's device {device}")
+        return device
+
+    def append(self, cache, K, V, pos):
+        """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds."""
+        if K.shape[1] != V.shape[1]:
+            raise SaError(1, "K and V must have the same number of rows")
+        h, device = self.cfg.n_kv_heads, self._own_cache(cache)
+        with self._current(device):
+            sa_cache_append(self.ctx, cache, _rows(K, h, device, "K"), _rows(V, h, device, "V"), K.shape[1], pos, self.stream())
+
+    def decode_cached(self, cache, q, pos, o):
+        """decode() with K and V out of a cache that holds tokens 0..pos."""
+        device, shape = self._own_cache(cache), (self.cfg.n_q_heads, 128)
+        for t in (q, o):
+            if tuple(t.shape) != shape or t.element_size() != 2 or not t.is_contiguous() or t.get_device() != device:
+                raise SaError(1, f"q and o must be contiguous 16-bit tensors {shape} on the session's device")
+        with self._current(device):
+            sa_cache_decode(self.ctx, cache, q, self._index(), pos, o, self.stream())
+
+    def attend_scratch(self):
+        """The session's scratch of attend(), allocated at the first use and kept."""
+        if self._attend_scratch is None:
+            size = sa_cache_attend_scratch_bytes(self.ctx)
+            raw = self.torch.empty(size + 256, dtype=self.torch.uint8, device=self.device)
+            off = (-raw.data_ptr()) % 256
+            self._attend_scratch = (raw, raw.data_ptr() + off, size)
+        return self._attend_scratch
+
+    def attend(self, cache, Q, pos, O):
+        """Causal attention of the newest tokens, Q and O [n_q_heads, n, 128], over a cache that holds pos + n."""
+        if Q.shape[1] != O.shape[1]:
+            raise SaError(1, "Q and O must have the same number of rows")
+        h, device = self.cfg.n_q_heads, self._own_cache(cache)
+        _, scratch, size = self.attend_scratch()
+        with self._current(device):
+            sa_cache_attend(self.ctx, cache, _rows(Q, h, device, "Q"), Q.shape[1], pos, _rows(O, h, device, "O"), scratch, size,
+                            self.stream())
 
     def search_patterns(self, Q, K, V, target_pairs, eps_pairs):
         """Alg. 1 on the scores of the last estimate(): one dict per head."""

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libsa_prefill.so")
-SOURCES = ["api.hip", "attn.hip", "estimate.hip", "index.hip", "search.hip", "decode.hip"]
+SOURCES = ["api.hip", "attn.hip", "estimate.hip", "index.hip", "search.hip", "decode.hip", "rotary.hip", "cache.hip",
+           "cache_decode.hip", "cache_attend.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", INCLUDE, "-I", CSRC]

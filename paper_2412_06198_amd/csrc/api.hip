@@ -354,6 +354,126 @@ sa_status sa_sparse_decode_static(sa_ctx *c, const void *q, const void *K, const
                                                 (hipStream_t)stream));
 }
 
+// A strided tensor of n rows a head: contiguous strides filled in, or why it cannot be taken.
+static const char *resolve_rows(sa_rows *r, int heads, int64_t n, bool output) {
+  if (!r->data) return "null pointer";
+  if ((uintptr_t)r->data & 15) return "tensors must be 16-byte aligned";
+  if (r->head_stride == 0 && r->row_stride == 0) {
+    r->row_stride = sa::kHeadDim;
+    r->head_stride = n * sa::kHeadDim;
+  }
+  const int64_t most = (int64_t)1 << 55;  // 128 heads and 2^31 rows of it stay addresses
+  // the stride of a single row or head is never used
+  if (heads == 1) r->head_stride = n * sa::kHeadDim;
+  if (n == 1 && r->row_stride <= 0) r->row_stride = sa::kHeadDim;
+  if (r->head_stride < sa::kHeadDim || r->row_stride < sa::kHeadDim || r->head_stride % 8 || r->row_stride % 8 ||
+      r->head_stride > most || r->row_stride > most >> 24)
+    return "strides must be multiples of 8, at least head_dim";
+  if (output && heads > 1 && n > 1) {
+    const bool rows_inside = r->head_stride / r->row_stride > n - 1 || (r->head_stride / r->row_stride == n - 1 && r->head_stride % r->row_stride >= sa::kHeadDim);
+    const bool heads_inside = r->row_stride / r->head_stride > heads - 1 || (r->row_stride / r->head_stride == heads - 1 && r->row_stride % r->head_stride >= sa::kHeadDim);
+    if (!rows_inside && !heads_inside) return "rows of an output overlap";
+  }
+  return nullptr;
+}
+
+sa_status sa_rotary_embed(sa_ctx *c, const sa_rotary *rotary, sa_rows Q, sa_rows K, int64_t n, int64_t pos,
+                          const int32_t *positions, sa_rows Q_out, sa_rows K_out, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (!rotary) return fail(c, SA_ERR_INVALID_ARG, "null pointer");
+  const int64_t top = (int64_t)1 << 31;
+  if (n < 0 || n > top || (!positions && (pos < 0 || pos > top - n)))
+    return fail(c, SA_ERR_INVALID_ARG, "0 <= pos and pos + n <= 2^31 are needed");
+  if ((uintptr_t)positions & 3) return fail(c, SA_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  if (n == 0) return SA_OK;  // an empty tensor may have no address
+  if (!Q.data && !K.data) return fail(c, SA_ERR_INVALID_ARG, "null pointer");
+  sa_rows *const in[2] = {&Q, &K}, *const out[2] = {&Q_out, &K_out};
+  for (int i = 0; i < 2; ++i) {
+    if (!in[i]->data) continue;
+    const int heads = i ? c->sh.Hkv : c->sh.Hq;
+    const char *why = resolve_rows(in[i], heads, n, false);
+    if (!why) why = resolve_rows(out[i], heads, n, true);
+    if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+    if (in[i]->data == out[i]->data && (in[i]->head_stride != out[i]->head_stride || in[i]->row_stride != out[i]->row_stride))
+      return fail(c, SA_ERR_INVALID_ARG, "in place, the strides must be the same");
+  }
+  return hip_result(c, sa::launch_rotary(c->sh, sa::rotary_table(rotary), Q, K, n, pos, positions, Q_out, K_out, (hipStream_t)stream));
+}
+
+sa_status sa_cache_bytes(const sa_ctx *c, int64_t capacity, size_t sizes[6]) {
+  if (!c || !sizes || capacity <= 0 || capacity % c->sh.b || capacity > (int64_t)1 << 30) return SA_ERR_INVALID_ARG;
+  const size_t heads = (size_t)c->sh.Hkv;
+  sizes[0] = sizes[1] = heads * (size_t)capacity * sa::kHeadDim;
+  sizes[2] = sizes[3] = heads * (size_t)(capacity / c->sh.b) * 4;
+  sizes[4] = sizes[5] = heads * (size_t)c->sh.b * sa::kHeadDim * 2;
+  return SA_OK;
+}
+
+static sa_status check_cache(sa_ctx *c, const sa_cache *h, int64_t tokens) {
+  if (!h || !h->k || !h->v || !h->k_scale || !h->v_scale || !h->k_open || !h->v_open)
+    return fail(c, SA_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)h->k | (uintptr_t)h->v | (uintptr_t)h->k_open | (uintptr_t)h->v_open) & 15)
+    return fail(c, SA_ERR_INVALID_ARG, "the cache's k, v, k_open, v_open must be 16-byte aligned");
+  if (((uintptr_t)h->k_scale | (uintptr_t)h->v_scale) & 3)
+    return fail(c, SA_ERR_INVALID_ARG, "the cache's scales must be 4-byte aligned");
+  if (h->type != SA_CACHE_E4M3 && h->type != SA_CACHE_E5M2) return fail(c, SA_ERR_INVALID_ARG, "unknown type of cache");
+  if (h->capacity <= 0 || h->capacity % c->sh.b || h->capacity > (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "the cache's capacity must be a multiple of block, at most 2^30");
+  if (tokens > h->capacity) return fail(c, SA_ERR_BUFFER_TOO_SMALL, "the cache has no room for that many tokens");
+  return SA_OK;
+}
+
+sa_status sa_cache_append(sa_ctx *c, const sa_cache *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (n < 0 || pos < 0 || n > (int64_t)1 << 30 || pos > (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "n and pos must lie in [0, 2^30]");
+  const sa_status s = check_cache(c, cache, pos + n);
+  if (s != SA_OK) return s;
+  if (n == 0) return SA_OK;
+  const char *why = resolve_rows(&K, c->sh.Hkv, n, false);
+  if (!why) why = resolve_rows(&V, c->sh.Hkv, n, false);
+  if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  return hip_result(c, sa::launch_cache_append(c->sh, *cache, K, V, n, pos, (hipStream_t)stream));
+}
+
+sa_status sa_cache_decode(sa_ctx *c, const sa_cache *cache, const void *q, sa_index idx, int64_t pos, void *o,
+                          void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (!q || !o || !idx.n_cols || !idx.cols || !idx.n_offs || !idx.offs || !idx.rowptr || !idx.blkcols)
+    return fail(c, SA_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)q | (uintptr_t)o) & 15) return fail(c, SA_ERR_INVALID_ARG, "q, o must be 16-byte aligned");
+  if (pos < c->sh.N || pos - c->sh.N >= (1 << 20))
+    return fail(c, SA_ERR_INVALID_ARG, "pos must lie in [seq_len, seq_len + 2^20)");
+  const sa_status s = check_cache(c, cache, pos + 1);
+  if (s != SA_OK) return s;
+  if (!c->have_ws) return fail(c, SA_ERR_INVALID_ARG, "no workspace attached");
+  return hip_result(c, sa::launch_cache_decode(c->sh, c->ws.dec_part, *cache, (const uint16_t *)q, idx, (int)pos,
+                                               (uint16_t *)o, (hipStream_t)stream));
+}
+
+sa_status sa_cache_attend_scratch_bytes(const sa_ctx *c, size_t *bytes) {
+  if (!c || !bytes) return SA_ERR_INVALID_ARG;
+  *bytes = sa::attend_scratch_bytes(c->sh);
+  return SA_OK;
+}
+
+sa_status sa_cache_attend(sa_ctx *c, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
+                          void *scratch, size_t scratch_bytes, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (n < 0 || pos < 0 || n > (int64_t)1 << 30 || pos > (int64_t)1 << 30 || n * c->sh.Hq >= (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
+  const sa_status s = check_cache(c, cache, pos + n);
+  if (s != SA_OK) return s;
+  if (!scratch || ((uintptr_t)scratch & 255)) return fail(c, SA_ERR_INVALID_ARG, "scratch must be a 256-byte aligned device pointer");
+  if (scratch_bytes < sa::attend_scratch_bytes(c->sh))
+    return fail(c, SA_ERR_BUFFER_TOO_SMALL, "scratch smaller than sa_cache_attend_scratch_bytes");
+  if (n == 0) return SA_OK;
+  const char *why = resolve_rows(&Q, c->sh.Hq, n, false);
+  if (!why) why = resolve_rows(&O, c->sh.Hq, n, true);
+  if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  return hip_result(c, sa::launch_cache_attend(c->sh, *cache, Q, (int)n, (int)pos, O, scratch, (hipStream_t)stream));
+}
+
 const char *sa_last_error(const sa_ctx *c) { return c ? c->err : "null context"; }
 
 }  // extern "C"

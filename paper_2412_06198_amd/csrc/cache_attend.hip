@@ -1,0 +1,506 @@
+// Causal attention of the newest n tokens over the 8-bit cache: O = softmax(scale Q K^T) V, row by row, with the running
+// maximum and sum of an online softmax, for n from one token to thousands.
+//
+// The g query heads of a KV head read the same keys, so its g n query rows (token, head of the group) are taken
+// together, 32 to a wave: a decode step of 8 heads a group fills 8 rows of one wave's products, a chunk of a prompt
+// fills workgroups of 128 rows.  Keys are walked in tiles.  Codes come from memory as they are, half the
+// bytes of bf16, and are turned into bf16 (exactly: code times a power of two) on their way into LDS, once per
+// workgroup; from there on it is the tile step of the sparse prefill: S^T = K Q^T with v_mfma_f32_32x32x16_bf16, so
+// that a lane owns a query row, and O^T += V^T P^T with transposing LDS reads.
+//
+// Two shapes of a workgroup (4 waves):
+//   many rows (WQ = 4)  each wave 32 of 128 rows, tiles of 64 keys shared by the four, two tiles in LDS in turn
+//   few rows (WQ = 1)   one set of up to 32 rows, each wave every fourth tile of 32 keys in LDS of its own, no barriers
+// and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
+// launch.
+#include <algorithm>
+
+#include "cache_codes.h"
+#include "sa_internal.h"
+
+namespace sa {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kThreads = 256;
+constexpr int kMaxSplits = 64;
+constexpr int kMasked = 4;  // tiles that some rows of a workgroup see and others do not: 128 keys and two ends at most
+constexpr int kRowsMany = 128, kRowsFew = 32;  // query rows of a workgroup
+
+struct AttendArgs {
+  const uint16_t *Q;
+  uint16_t *O;
+  const uint8_t *K, *V;
+  const float *k_scale, *v_scale;
+  const uint16_t *k_open, *v_open;
+  int64_t q_hs, q_rs, o_hs, o_rs, capacity;
+  int g, Hkv, rows, tiles, S;  // query heads and query rows of a KV head, row tiles, splits of the keys
+  int shift;                   // log2 of the block
+  int pos, tokens, closed;     // of the first query; in the cache; in its full blocks
+  float c;                     // softmax scale * log2(e)
+  float *part;                 // [Hkv * rows][S][128] unnormalised outputs of the splits
+  float2 *ml;                  // [Hkv * rows][S] their maxima and sums
+};
+
+__device__ inline float max_pair(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ inline float sum_pair(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// 16 codes of a row, 8 words of bf16.
+template <int TYPE>
+__device__ inline void decode16(const uint4 x, float scale, uint4 &lo, uint4 &hi) {
+  lo.x = decode2<TYPE, false>(x.x, scale); lo.y = decode2<TYPE, true>(x.x, scale);
+  lo.z = decode2<TYPE, false>(x.y, scale); lo.w = decode2<TYPE, true>(x.y, scale);
+  hi.x = decode2<TYPE, false>(x.z, scale); hi.y = decode2<TYPE, true>(x.z, scale);
+  hi.z = decode2<TYPE, false>(x.w, scale); hi.w = decode2<TYPE, true>(x.w, scale);
+}
+
+// Whether a pair of bf16 values holds an infinity or NaN; and the pair without it.
+__device__ inline uint32_t nonfinite(uint32_t w) { return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u; }
+__device__ inline uint32_t finite_only(uint32_t w) {
+  const uint32_t bad = nonfinite(w);
+  return w & ~((bad << 1) - (bad >> 15));
+}
+
+__device__ inline void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ inline float value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+// Element d of key j of K or V, as the cache has it.
+template <int TYPE>
+__device__ inline float element(const AttendArgs &p, int kvh, const uint8_t *codes, const float *scale, const uint16_t *open, int j, int d) {
+  if (j >= p.closed) return value(open[(((size_t)kvh << p.shift) + (j - p.closed)) * kHeadDim + d]);
+  return decode2f<TYPE, false>(codes[((size_t)kvh * p.capacity + j) * kHeadDim + d])[0] * scale[(size_t)kvh * (p.capacity >> p.shift) + (j >> p.shift)];
+}
+
+template <int TYPE, int WQ>
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs p) {
+  constexpr int WK = 4 / WQ;            // groups of waves that walk keys of their own
+  constexpr int KT = WQ == 4 ? 64 : 32; // keys per tile
+  constexpr int HF = KT / 32;
+  constexpr int NBUF = WQ == 4 ? 2 : 1;
+  constexpr int GT = 64 * WQ;           // threads of a group
+  constexpr int NC = KT * 8 / GT;       // 16-byte pieces of codes of K, and of V, that a thread stages per tile
+  __shared__ __attribute__((aligned(16))) uint16_t lds[WK][NBUF][2][KT * 128];
+  __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles whose V has an infinity or NaN
+  __shared__ float s_m[4][32], s_l[4][32];
+
+  const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = WQ == 4 ? 0 : wave, wq = WQ == 4 ? wave : 0, gt = WQ == 4 ? tid : lane;
+
+  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then
+  // row tiles from the last one (the most keys) down.
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, rt = p.tiles - 1 - rest / p.S;
+  const int r0 = rt * 32 * WQ, r_last = min(r0 + 32 * WQ, p.rows) - 1;
+  const int seen_all = p.pos + r0 / p.g;                           // last key that every row of the workgroup sees
+  const int t_masked = (seen_all + 1) / KT;                        // first tile that some do not
+  const int n_tiles = (p.pos + r_last / p.g) / KT + 1;          // tiles that some row sees
+  const int per = (n_tiles + p.S - 1) / p.S;
+  const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
+  const int n_closed = p.closed / KT;
+
+  // this lane's row, and the last keys that it, its wave's first and its wave's last row see
+  const int wr0 = min(r0 + 32 * wq, p.rows - 1), wr1 = min(r0 + 32 * wq + 31, p.rows - 1);
+  const int row = min(r0 + 32 * wq + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g);
+  const int see = p.pos + tok, see0 = p.pos + wr0 / p.g, see1 = p.pos + wr1 / p.g;
+
+  const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim;
+  const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim;
+  const float *ksh = p.k_scale + (size_t)kvh * (p.capacity >> p.shift), *vsh = p.v_scale + (size_t)kvh * (p.capacity >> p.shift);
+
+  bf16x8 qf[8];  // Q^T fragments: B operand, lane = query row, 8 consecutive d per k-step half
+  {
+    const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 16 * ks + 8 * gg);
+  }
+  f32x16 oacc[4];
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+  float m_run = -INFINITY;
+  f32x4 lacc[2] = {};
+
+  // ---- staging: codes into registers, a tile ahead; then as bf16 into LDS ----------------------------
+  uint4 kc[NC], vc[NC];
+  float ksc = 1.f, vsc = 1.f;
+  auto fetch = [&](int t) {
+    if (t < n_closed) {
+      const size_t at = (size_t)t * KT * kHeadDim + gt * 16;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        kc[i] = *(const uint4 *)(Kh + at + (size_t)i * GT * 16);
+        vc[i] = *(const uint4 *)(Vh + at + (size_t)i * GT * 16);
+      }
+      const int blk = (t * KT) >> p.shift;
+      ksc = ksh[blk];
+      vsc = vsh[blk];
+    }
+  };
+  // LDS tiles are KT rows x 256 B, the 16-byte chunks of a row XOR-swizzled: K chunk c of row r at c ^ (r & 15) (b128
+  // reads of 16 rows hit 64 banks), V chunk c at c ^ ((r & 3) << 2) (the transposing b64 reads do).
+  auto put_row = [&](uint16_t *tile, int r, int c16, int swz, const uint4 &lo, const uint4 &hi) {
+    char *at = (char *)tile + r * 256;
+    *(uint4 *)(at + (((2 * c16) ^ swz) << 4)) = lo;
+    *(uint4 *)(at + (((2 * c16 + 1) ^ swz) << 4)) = hi;
+  };
+  auto stage = [&](int t, int buf) {
+    const int j0 = t * KT;
+    const bool masked = t >= t_masked;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int id = gt + i * GT, r = id >> 3, c16 = id & 7;
+      uint4 klo, khi, vlo, vhi;
+      if (t < n_closed) {
+        decode16<TYPE>(kc[i], ksc, klo, khi);
+        decode16<TYPE>(vc[i], vsc, vlo, vhi);
+      } else {  // the open block: bf16 rows, zeros behind the tokens
+        klo = khi = vlo = vhi = make_uint4(0u, 0u, 0u, 0u);
+        if (j0 + r < p.tokens) {
+          const size_t at = (((size_t)kvh << p.shift) + (size_t)(j0 + r - p.closed)) * kHeadDim + c16 * 16;
+          klo = *(const uint4 *)(p.k_open + at);
+          khi = *(const uint4 *)(p.k_open + at + 8);
+          vlo = *(const uint4 *)(p.v_open + at);
+          vhi = *(const uint4 *)(p.v_open + at + 8);
+        }
+      }
+      if (masked) {
+        // A row that does not see a key gives it weight 0, and 0 x inf is not 0: non-finite values of V
+        // stay out of the products here and come back at the end for the rows that do see them.
+        const uint32_t bad = nonfinite(vlo.x) | nonfinite(vlo.y) | nonfinite(vlo.z) | nonfinite(vlo.w) |
+                             nonfinite(vhi.x) | nonfinite(vhi.y) | nonfinite(vhi.z) | nonfinite(vhi.w);
+        const uint64_t who = __ballot(bad != 0u);
+        if (c16 == 0) rowbad[(t - t_masked) * KT + r] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
+        vlo = make_uint4(finite_only(vlo.x), finite_only(vlo.y), finite_only(vlo.z), finite_only(vlo.w));
+        vhi = make_uint4(finite_only(vhi.x), finite_only(vhi.y), finite_only(vhi.z), finite_only(vhi.w));
+      }
+      put_row(lds[grp][buf][0], r, c16, r & 15, klo, khi);
+      put_row(lds[grp][buf][1], r, c16, (r & 3) << 2, vlo, vhi);
+    }
+  };
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const unsigned kbase = (unsigned)(q * 256) | (unsigned)((q & 15) << 4);
+  unsigned vbase;
+  {
+    const int r = lane & 15, part = (lane >> 4) & 1, vrow = 4 * gg + (r >> 2);
+    vbase = (unsigned)(vrow * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vrow & 3) << 2)) << 4) | (unsigned)((r & 1) << 3);
+  }
+#define SA_KFRAG(tile, hf, ks) \
+  (*(const bf16x8 *)((const char *)(tile) + ((kbase ^ (unsigned)((2 * (ks) + gg) << 4)) + (hf) * 32 * 256)))
+#define SA_VTR(tile, db, key0) \
+  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6)) + (key0) * 256)))
+
+  auto attend = [&](int t, int buf) {
+    const int j0 = t * KT;
+    if (j0 > see1) return;
+    const bool needmask = j0 + KT - 1 > see0;
+    const int lim = see - j0 - 4 * gg;  // slot c of this lane is kept iff c <= lim
+    const uint16_t *Kt = lds[grp][buf][0], *Vt = lds[grp][buf][1];
+    // ---- S^T = K Q^T: lane = query row (q), accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4
+    f32x16 sacc[HF];
+#pragma unroll
+    for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[hf][r] = 0.f;
+    {
+      bf16x8 kf[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kf[i] = SA_KFRAG(Kt, i % HF, i / HF);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 8 * HF; ++i) {
+        const int hf = i % HF, ks = i / HF;
+        sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[ks], sacc[hf], 0, 0, 0);
+        if (i + 4 < 8 * HF) kf[i & 3] = SA_KFRAG(Kt, (i + 4) % HF, (i + 4) / HF);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (needmask) {
+#pragma unroll
+      for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int c = 32 * hf + 8 * (r / 4) + (r % 4);
+          if (c > lim) sacc[hf][r] = -INFINITY;
+        }
+    }
+    __builtin_amdgcn_s_setprio(0);
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[hf][r]);
+    tmax = max_pair(tmax);
+    const float m_new = fmaxf(m_run, tmax * p.c);
+    // The reference moves only when some row's maximum grew by more than 2^8: until then probabilities may exceed 1
+    // (by at most 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
+    if (__any(m_new - m_run > 8.f)) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run - ((m_new == -INFINITY) ? 0.f : m_new));
+      m_run = m_new;
+      lacc[0] *= alpha;
+      lacc[1] *= alpha;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+    }
+    const float m_ref = (m_run == -INFINITY) ? 0.f : m_run;
+    // ---- probabilities, a pair at a time, beside the products: see the sparse prefill for the order -----------
+    auto soft2 = [&](int g, int j) {
+#pragma unroll
+      for (int e = 2 * j; e < 2 * j + 2; ++e)
+        sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[g >> 1][8 * (g & 1) + e], p.c, -m_ref));
+    };
+    u32x4 pbuf[2];
+    auto cvt2 = [&](int g, int j) {
+      const bf16x2 pr = {(__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j], (__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j + 1]};
+      pbuf[g & 1][j] = __builtin_bit_cast(uint32_t, pr);
+    };
+    // The normaliser sums the probabilities as rounded to bf16, so that a row stays a convex combination of its V rows;
+    // 4x4x4 products with ones do it on the matrix pipe.
+    const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+    constexpr int kProducts = 8 * HF;  // HF * 2 key steps x 4 d blocks
+    s16x4 vlo[4], vhi[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) soft2(0, j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      vlo[i] = SA_VTR(Vt, i & 3, 16 * (i >> 2));
+      vhi[i] = SA_VTR(Vt, i & 3, 16 * (i >> 2) + 8);
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) cvt2(0, j);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {
+      const int g = i >> 2, db = i & 3;
+      if (db == 0) {
+        cvt2(g, 3);
+        asm("" : "+v"(pbuf[g & 1]));
+      }
+      const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1]);
+      const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
+      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
+      const s16x8 ps = __builtin_bit_cast(s16x8, pb);
+      if (db == 0)
+        lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+      if (db == 3)
+        lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+      if (i + 4 < kProducts) {
+        vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
+        vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
+      }
+      if (g + 1 < 2 * HF) {
+        soft2(g + 1, db);
+        if (db > 0) cvt2(g + 1, db - 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if constexpr (WQ == 4) {
+    if (t_begin < t_end) {
+      fetch(t_begin);
+      stage(t_begin, 0);
+      if (t_begin + 1 < t_end) fetch(t_begin + 1);
+      for (int t = t_begin; t < t_end; ++t) {
+        const int cur = (t - t_begin) & 1;
+        __syncthreads();  // tile t is in LDS, and every wave is done with tile t - 1
+        if (t + 1 < t_end) stage(t + 1, cur ^ 1);
+        if (t + 2 < t_end) fetch(t + 2);
+        attend(t, cur);
+      }
+    }
+  } else {
+    if (t_begin + grp < t_end) fetch(t_begin + grp);
+    for (int t = t_begin + grp; t < t_end; t += WK) {
+      stage(t, 0);
+      wave_lds_sync();
+      if (t + WK < t_end) fetch(t + WK);
+      attend(t, 0);
+      wave_lds_sync();
+    }
+  }
+  // Non-finite values of V in tiles that only some rows see: their share, for the rows that do.  Seldom there, so the
+  // scores are taken once more, plainly.
+  if (t_end > t_masked) {
+    __syncthreads();
+    const int base = max(t_begin, t_masked) * KT;
+    for (int j = base; j < t_end * KT; ++j) {
+      if (!__builtin_amdgcn_readfirstlane(rowbad[j - t_masked * KT]) || j >= p.tokens) continue;
+      if (WQ == 1 && (j / KT - t_begin) % WK != grp) continue;  // another wave's tile
+      float s = 0.f;
+      for (int d = 0; d < kHeadDim; ++d)
+        s = __builtin_fmaf(value(p.Q[(size_t)head * p.q_hs + (size_t)tok * p.q_rs + d]), element<TYPE>(p, kvh, p.K, p.k_scale, p.k_open, j, d), s);
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, p.c, m_run == -INFINITY ? 0.f : -m_run));
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float v = element<TYPE>(p, kvh, p.V, p.v_scale, p.v_open, j, 32 * db + 8 * (r / 4) + 4 * gg + r % 4);
+          if (j <= see && !__builtin_isfinite(v)) oacc[db][r] += w * v;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
+  const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
+
+  // ---- out: O / l in bf16, or the split's sums ------------------------------------------------------
+  if constexpr (WQ == 4) {
+    const bool mine = r0 + 32 * wq + q < p.rows;
+    const size_t slot = ((size_t)kvh * p.rows + row) * p.S + sp;
+    if (mine && p.S > 1) {
+      if (gg == 0) p.ml[slot] = make_float2(m_run, l_run);
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *(float4 *)(p.part + slot * kHeadDim + 32 * db + 2 * r + 4 * gg) =
+              make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
+    } else if (mine) {
+      const float inv = 1.f / l_run;
+      uint16_t *o = p.O + (size_t)head * p.o_hs + (size_t)tok * p.o_rs;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const bf16x2 a = {(__bf16)(oacc[db][r] * inv), (__bf16)(oacc[db][r + 1] * inv)};
+          const bf16x2 b = {(__bf16)(oacc[db][r + 2] * inv), (__bf16)(oacc[db][r + 3] * inv)};
+          *(uint2 *)(o + 32 * db + 2 * r + 4 * gg) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+        }
+    }
+  } else {
+    // the four waves' sums of the same rows, through the LDS of the tiles
+    float *const so = (float *)&lds[0][0][0][0];  // [4][32][128]
+    static_assert(sizeof(lds) >= 4 * 32 * 128 * 4, "holds the waves' outputs");
+    __syncthreads();
+    if (gg == 0) { s_m[wave][q] = m_run; s_l[wave][q] = l_run; }
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(float4 *)(so + (wave * 32 + q) * kHeadDim + ((32 * db + 2 * r + 4 * gg) ^ ((q & 7) << 2))) =
+            make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
+    __syncthreads();
+    const int mr = tid >> 3, d0 = (tid & 7) * 16;  // 16 outputs of a row each
+    const int orow = r0 + mr;
+    if (orow < p.rows) {
+      float M = -INFINITY, L = 0.f, w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) M = fmaxf(M, s_m[k][mr]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[k] = s_m[k][mr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][mr] - M);
+        L += s_l[k][mr] * w[k];
+      }
+      const size_t slot = ((size_t)kvh * p.rows + orow) * p.S + sp;
+      const float inv = p.S > 1 ? 1.f : 1.f / L;
+      const int otok = orow / p.g;
+      uint16_t *o = p.O + (size_t)(kvh * p.g + orow - otok * p.g) * p.o_hs + (size_t)otok * p.o_rs;
+      if (p.S > 1 && d0 == 0) p.ml[slot] = make_float2(M, L);
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 x = *(const float4 *)(so + (k * 32 + mr) * kHeadDim + ((d0 + i) ^ ((mr & 7) << 2)));
+          a.x = __builtin_fmaf(x.x, w[k], a.x); a.y = __builtin_fmaf(x.y, w[k], a.y);
+          a.z = __builtin_fmaf(x.z, w[k], a.z); a.w = __builtin_fmaf(x.w, w[k], a.w);
+        }
+        if (p.S > 1) {
+          *(float4 *)(p.part + slot * kHeadDim + d0 + i) = a;
+        } else {
+          const bf16x2 u = {(__bf16)(a.x * inv), (__bf16)(a.y * inv)}, v = {(__bf16)(a.z * inv), (__bf16)(a.w * inv)};
+          *(uint2 *)(o + d0 + i) = make_uint2(__builtin_bit_cast(uint32_t, u), __builtin_bit_cast(uint32_t, v));
+        }
+      }
+    }
+  }
+}
+
+// The splits of a row joined: a wave per row, two outputs a lane.
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);  // KV head, row
+  if (at >= (int64_t)p.Hkv * p.rows) return;
+  const float2 ml = lane < p.S ? p.ml[at * p.S + lane] : make_float2(-INFINITY, 0.f);
+  float M = ml.x;
+  for (int e = 32; e >= 1; e >>= 1) M = fmaxf(M, __shfl_xor(M, e));
+  const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+  float L = ml.y * w;
+  for (int e = 32; e >= 1; e >>= 1) L += __shfl_xor(L, e);
+  float2 o = make_float2(0.f, 0.f);
+  for (int s = 0; s < p.S; ++s) {
+    const float ws = __shfl(w, s);
+    const float2 x = *(const float2 *)(p.part + (at * p.S + s) * kHeadDim + 2 * lane);
+    o.x = __builtin_fmaf(x.x, ws, o.x);
+    o.y = __builtin_fmaf(x.y, ws, o.y);
+  }
+  const int kvh = (int)(at / p.rows), row = (int)(at - (int64_t)kvh * p.rows), tok = row / p.g;
+  const bf16x2 r = {(__bf16)(o.x / L), (__bf16)(o.y / L)};
+  *(uint32_t *)(p.O + (size_t)(kvh * p.g + row - tok * p.g) * p.o_hs + (size_t)tok * p.o_rs + 2 * lane) = __builtin_bit_cast(uint32_t, r);
+}
+
+// Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit.
+size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
+
+}  // namespace
+
+size_t attend_scratch_bytes(const Shape &sh) { return max_slots(sh) * (kHeadDim * 4 + 8); }
+
+hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, int n, int pos, sa_rows O,
+                               void *scratch, hipStream_t st) {
+  AttendArgs a;
+  a.Q = (const uint16_t *)Q.data; a.O = (uint16_t *)O.data;
+  a.K = (const uint8_t *)c.k; a.V = (const uint8_t *)c.v; a.k_scale = c.k_scale; a.v_scale = c.v_scale;
+  a.k_open = (const uint16_t *)c.k_open; a.v_open = (const uint16_t *)c.v_open;
+  a.q_hs = Q.head_stride; a.q_rs = Q.row_stride; a.o_hs = O.head_stride; a.o_rs = O.row_stride;
+  a.capacity = c.capacity;
+  a.g = sh.g; a.Hkv = sh.Hkv; a.rows = sh.g * n;
+  a.shift = sh.b == 128 ? 7 : 6;
+  a.pos = pos; a.tokens = pos + n; a.closed = a.tokens >> a.shift << a.shift;
+  a.c = sh.scale * 1.4426950408889634f;
+  const bool few = a.rows <= kRowsFew;
+  const int per_wg = few ? kRowsFew : kRowsMany;
+  a.tiles = (a.rows + per_wg - 1) / per_wg;
+  // Splits of the keys: two workgroups a compute unit in all, 128 (few rows) or 256 keys a workgroup at least.
+  const int64_t wgs = (int64_t)a.tiles * sh.Hkv;
+  int64_t S = 2 * (int64_t)sh.n_cu / wgs;
+  S = std::min<int64_t>(S, (a.tokens + (few ? 127 : 255)) / (few ? 128 : 256));
+  S = std::min<int64_t>(S, (int64_t)(max_slots(sh) / ((size_t)a.rows * sh.Hkv)));
+  a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
+  a.ml = (float2 *)scratch;
+  a.part = (float *)((char *)scratch + max_slots(sh) * 8);
+  const unsigned grid = (unsigned)(wgs * a.S);
+  if (c.type == SA_CACHE_E4M3) {
+    if (few) attend_kernel<SA_CACHE_E4M3, 1><<<grid, kThreads, 0, st>>>(a);
+    else attend_kernel<SA_CACHE_E4M3, 4><<<grid, kThreads, 0, st>>>(a);
+  } else {
+    if (few) attend_kernel<SA_CACHE_E5M2, 1><<<grid, kThreads, 0, st>>>(a);
+    else attend_kernel<SA_CACHE_E5M2, 4><<<grid, kThreads, 0, st>>>(a);
+  }
+  if (a.S > 1) {
+    const int64_t all = (int64_t)sh.Hkv * a.rows;
+    join_kernel<<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace sa

@@ -16,12 +16,11 @@
 #include <atomic>
 #include <mutex>
 
+#include "decode_common.h"
 #include "sa_internal.h"
 
 namespace sa {
 namespace {
-
-constexpr int kPartStride = 132;  // floats per partial: max, sum, 2 (first one: arrival counter, others: 0), 128 outputs
 
 // Partials of the variant that allocates nothing (sa_sparse_decode_static): room for the largest
 // head count x split count the launcher ever picks (Hq * splits <= 512), 270336 bytes on every GPU
@@ -30,17 +29,6 @@ constexpr int kPartStride = 132;  // floats per partial: max, sum, 2 (first one:
 constexpr int kStaticPartials = 512;
 static __device__ __align__(256) float scratch[kStaticPartials * kPartStride];
 constexpr int kMaxDevices = 64;
-
-// A head's arrival counter lives in floats 2 and 3 of its first partial: the step's token in the upper 48
-// bits, in the lower 16 the number of workgroups that have arrived.  The memory may hold anything: what the
-// caller's workspace was used for before, or the count of a step that overlapped another one or never ended.
-// A step takes only its own token for a count: a head's first workgroup puts the token there while its rows are
-// on their way, one that arrives before that does it itself, and nothing is read from what was left.  Each
-// launch has a token of its own, so that no clearing launch is needed; a recorded one repeats its token with
-// every replay, so there the counters are cleared by a launch before it (8 heads, 4096 tokens: 8.4 us a
-// recorded step instead of 6.6; a count that the last one to arrive put back to 0 cost 0.1 us less, and what an
-// overlapping step left there stayed for good).
-constexpr int kCountBits = 16;
 
 struct DecArgs {
   const uint16_t *q, *K, *V;
@@ -59,85 +47,13 @@ constexpr int kStep = 4 * U;  // keys of a wave per step: four slots of 16 lanes
 constexpr int kRing = 128;    // keys of a wave that are resolved and not yet read: 15 + 64 at most
 constexpr int kMinChunk = kWaves * kStep;  // keys of a workgroup: one step of each wave; 128 was 0.7 us slower
 
-// A reduction over the four 16-lane slots of a wave, on each lane.
-template <typename F>
-__device__ inline float over_slots(float x, F f) {
-  const unsigned a = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  const unsigned r0 = r[0], r1 = r[1];
-  const unsigned c = __float_as_uint(f(__uint_as_float(r0), __uint_as_float(r1)));
-  const auto s = __builtin_amdgcn_permlane32_swap(c, c, false, false);
-  const unsigned s0 = s[0], s1 = s[1];
-  return f(__uint_as_float(s0), __uint_as_float(s1));
-}
-
-__device__ inline void unpack8(const uint4 x, float (&f)[8]) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = __uint_as_float(w[e] << 16);
-    f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-  }
-}
-
 // Sum over 16 lanes, on each of them: partners at distance 8, 7, 2 and 1.
-template <int CTRL>
-__device__ inline float row_move(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
-}
 __device__ inline float sum16(float x) {
   x += row_move<0x128>(x);
   x += row_move<0x141>(x);
   x += row_move<0x4E>(x);
   x += row_move<0xB1>(x);
   return x;
-}
-
-// Partial results cross workgroups inside the launch by agent-scope accesses, which pass the L2 caches
-// by: nothing has to be written back or invalidated on the way (fences at that scope cost 40 us here).  They
-// are ordered before the arrival by vmcnt(0) and the workgroup's barrier, see the top of index.hip.
-__device__ inline void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ inline float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
-// Merge n <= 64 partials of a head, normalise, round to bf16: 256 threads, thread (k0, d) takes the outputs d
-// of partials k0, k0 + 2, ...  All reads are on their way before the first is needed.
-__device__ inline void merge(const float *src, int n, float *wgt, float *s_L, float *half, uint16_t *o) {
-  const int tid = threadIdx.x, d = tid & 127, k0 = tid >> 7;
-  float mk = -INFINITY, lk = 0.f;
-  if (tid < n) {
-    mk = get(src + (size_t)tid * kPartStride);
-    lk = get(src + (size_t)tid * kPartStride + 1);
-  }
-  float x[32];
-  // Places past the end weigh 0 and read the 0 that the last partial holds for them: anything else could be
-  // infinite.  (Masks on x after the reads cost 0.3 us.)
-  const int none = (n - 1) * kPartStride + 2;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    if (8 * (i / 8) * 2 < n) x[i] = get(src + (k0 + 2 * i < n ? (k0 + 2 * i) * kPartStride + 4 + d : none));  // by eights
-    else x[i] = 0.f;
-  }
-  if (tid < 64) {
-    float M = mk;
-    for (int e = 32; e >= 1; e >>= 1) M = fmaxf(M, __shfl_xor(M, e));
-    const float w = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - M);
-    float L = lk * w;
-    for (int e = 32; e >= 1; e >>= 1) L += __shfl_xor(L, e);
-    wgt[tid] = w;  // 0 from n on
-    if (tid == 0) *s_L = L;
-  }
-  __syncthreads();
-  float O = 0.f;
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    O = __builtin_fmaf(x[i], wgt[k0 + 2 * i], O);
-  if (k0) half[d] = O;
-  __syncthreads();
-  if (k0) return;
-  O += half[d];
-  const float L = *s_L;
-  const __bf16 r = (__bf16)(L > 0.f ? O / L : 0.f);
-  o[d] = __builtin_bit_cast(uint16_t, r);
 }
 
 // A head's key list, in this order: keys of the kept blocks, columns, diagonal keys, generated keys; and how
@@ -159,12 +75,6 @@ __device__ inline KeyList key_list(const DecArgs &p, int h) {
   k.chunk = max(((k.total + p.S - 1) / p.S + 15) / 16 * 16, kMinChunk);
   k.n = (k.total + k.chunk - 1) / k.chunk;  // <= S, and at least 1: the query's own key is in the list
   return k;
-}
-
-// What one lane has written to LDS before is read by the others of its wave after it, and the other way round.
-__device__ inline void wave_lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 // grid (S, Hq), 256 threads.  Each wave walks a quarter of the workgroup's keys by itself: 64 lanes resolve 64
@@ -304,9 +214,7 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(DecArgs p) {
   if (resolve()) {
     fetch(kx[0], vx[0], cnt[0]);
     // the token into the counter, unless a workgroup of this step has been there
-    if (claims && (seen ^ p.token) >> kCountBits)
-      (void)__hip_atomic_compare_exchange_strong(arrived, &seen, p.token, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                 __HIP_MEMORY_SCOPE_AGENT);
+    if (claims) claim(arrived, seen, p.token);
     for (;;) {
       const bool more = resolve();
       if (more) fetch(kx[1], vx[1], cnt[1]);
@@ -360,33 +268,19 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(DecArgs p) {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this thread's partials have been performed
   __syncthreads();
   if (counts) {
-    uint64_t before = __hip_atomic_fetch_add(arrived, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    while ((before ^ p.token) >> kCountBits) {  // added to a value that is not this step's: nobody has been here yet
-      uint64_t cur = before + 1;                // ends: an exchange only fails where a workgroup has changed the counter
-      if (__hip_atomic_compare_exchange_strong(arrived, &cur, p.token + 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                               __HIP_MEMORY_SCOPE_AGENT))
-        before = p.token;  // this one put the token there, and itself
-      else if ((cur ^ p.token) >> kCountBits)
-        before = cur - 1;
-      else
-        before = __hip_atomic_fetch_add(arrived, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    s_last = before == p.token + (uint64_t)(L.n - 1);
+    s_last = arrive(arrived, p.token, L.n);
   }
   __syncthreads();
   asm volatile("" ::: "memory");
   if (s_last) merge(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
 }
 
-// The arrival counters of all heads, before a recorded step.
-__global__ void clear_arrivals_kernel(float *part, int Hq, int S) {
-  if ((int)threadIdx.x < Hq) *(uint64_t *)(part + (size_t)threadIdx.x * S * kPartStride + 2) = 0;
-}
+}  // namespace
 
 // 48 bits that no launch of the process has had before: a count times an odd number, so that they are neither a
 // neighbour of an earlier token nor a value that other data is likely to hold.  (2^48 launches come around
 // after 28 years at one every 3 us.)
-uint64_t next_token() {
+uint64_t next_decode_token() {
   static std::atomic<uint64_t> launches{0};
   for (;;) {
     const uint64_t t = (launches.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9D37C1E5A86B4F01ull << kCountBits;
@@ -394,7 +288,15 @@ uint64_t next_token() {
   }
 }
 
-}  // namespace
+// If the stream cannot say, the step is launched as a recorded one: right in either case.
+bool decode_recorded(hipStream_t st) {
+  hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &recording) != hipSuccess) {
+    (void)hipGetLastError();
+    recording = hipStreamCaptureStatusActive;
+  }
+  return recording != hipStreamCaptureStatusNone;
+}
 
 int decode_splits(const Shape &sh) {
   const int s = 512 / (sh.Hq > 0 ? sh.Hq : 1);  // about two workgroups per compute unit in all
@@ -452,14 +354,8 @@ hipError_t launch_sparse_decode(const Shape &sh, float *partials, const uint16_t
   a.cap_b = sh.cap_b; a.S = splits_of_step(sh, pos); a.pos = pos;
   a.kv_hs = sh.kv_hs; a.kv_rs = sh.kv_rs;
   a.c = sh.scale * 1.4426950408889634f;
-  a.token = next_token();
-  hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
-  // if the stream cannot say, the step is launched as a recorded one: right in either case
-  if (hipStreamIsCapturing(st, &recording) != hipSuccess) {
-    (void)hipGetLastError();
-    recording = hipStreamCaptureStatusActive;
-  }
-  if (recording != hipStreamCaptureStatusNone) clear_arrivals_kernel<<<1, kMaxHeads, 0, st>>>(partials, sh.Hq, a.S);
+  a.token = next_decode_token();
+  if (decode_recorded(st)) clear_arrivals_kernel<<<1, kMaxHeads, 0, st>>>(partials, sh.Hq, a.S);
   decode_kernel<<<dim3(a.S, sh.Hq), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }

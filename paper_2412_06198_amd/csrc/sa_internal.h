@@ -126,8 +126,23 @@ size_t attn_tile_bytes(const Shape &sh);
 // partials: decode_partial_bytes(sh) bytes of device memory (the context's workspace, or the static array)
 hipError_t launch_sparse_decode(const Shape &sh, float *partials, const uint16_t *q, const uint16_t *K,
                                 const uint16_t *V, sa_index idx, int pos, uint16_t *o, hipStream_t st);
+int decode_splits(const Shape &sh);                 // partials of a head that decode_partial_bytes has room for
+uint64_t next_decode_token();                       // of one launch, see decode_common.h
+bool decode_recorded(hipStream_t st);               // whether the stream is being captured
 size_t decode_static_bytes();                       // size of the library's static decode scratch
 hipError_t decode_static_scratch(float **out);      // its address on the current device
+// Frequencies of the pairs as fractions (of 2^64) of a turn per position, and the factors of sine and cosine.
+struct RotaryTable { uint64_t turn[64]; float sine, cosine; int pairs, layout; };
+const RotaryTable &rotary_table(const sa_rotary *r);
+hipError_t launch_rotary(const Shape &sh, const RotaryTable &f, sa_rows Q, sa_rows K, int64_t n, int64_t pos,
+                         const int32_t *positions, sa_rows Qo, sa_rows Ko, hipStream_t st);
+hipError_t launch_cache_append(const Shape &sh, const sa_cache &c, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                               hipStream_t st);
+hipError_t launch_cache_decode(const Shape &sh, float *partials, const sa_cache &c, const uint16_t *q, sa_index idx,
+                               int pos, uint16_t *o, hipStream_t st);
+size_t attend_scratch_bytes(const Shape &sh);
+hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, int n, int pos, sa_rows O,
+                               void *scratch, hipStream_t st);
 hipError_t launch_sparse_prefill(const Shape &sh, const Workspace &ws, const uint16_t *Q,
                                  const uint16_t *K, const uint16_t *V, sa_index idx, uint16_t *O,
                                  unsigned long long *counters, hipStream_t st);
