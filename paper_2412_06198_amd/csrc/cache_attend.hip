@@ -14,6 +14,7 @@
 // and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
 // launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_codes.h"
 #include "sa_internal.h"
@@ -28,10 +29,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
 constexpr int kMaxSplits = 64;
-constexpr int kMasked = 4;  // tiles that some rows of a workgroup see and others do not: 128 keys and two ends at most
 constexpr int kRowsMany = 128, kRowsFew = 32;  // query rows of a workgroup
 
 struct AttendArgs {
@@ -88,37 +90,167 @@ __device__ inline float element(const AttendArgs &p, int kvh, const uint8_t *cod
   return decode2f<TYPE, false>(codes[((size_t)kvh * p.capacity + j) * kHeadDim + d])[0] * scale[(size_t)kvh * (p.capacity >> p.shift) + (j >> p.shift)];
 }
 
-template <int TYPE, int WQ>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs p) {
-  constexpr int WK = 4 / WQ;            // groups of waves that walk keys of their own
-  constexpr int KT = WQ == 4 ? 64 : 32; // keys per tile
-  constexpr int HF = KT / 32;
-  constexpr int NBUF = WQ == 4 ? 2 : 1;
-  constexpr int GT = 64 * WQ;           // threads of a group
-  constexpr int NC = KT * 8 / GT;       // 16-byte pieces of codes of K, and of V, that a thread stages per tile
-  __shared__ __attribute__((aligned(16))) uint16_t lds[WK][NBUF][2][KT * 128];
+// A read-only word at a wave-uniform address.
+__device__ inline float uniform_load(const float *p, int i) {
+  typedef const float __attribute__((address_space(4))) *const_f32p;
+  return ((const_f32p)(uintptr_t)p)[i];
+}
+
+// The non-finite values of V of key j, which the products have been kept from, added for a lane's row if it sees the key.
+// Seldom there, so the score is taken once more, plainly.
+template <int TYPE>
+__device__ inline void add_nonfinite(const AttendArgs &p, int kvh, int j, int head, int tok, int see, int gg, float m, f32x16 (&o)[4]) {
+  float s = 0.f;
+  for (int d = 0; d < kHeadDim; ++d)
+    s = __builtin_fmaf(value(p.Q[(size_t)head * p.q_hs + (size_t)tok * p.q_rs + d]), element<TYPE>(p, kvh, p.K, p.k_scale, p.k_open, j, d), s);
+  const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, p.c, m == -INFINITY ? 0.f : -m));
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float v = element<TYPE>(p, kvh, p.V, p.v_scale, p.v_open, j, 32 * db + 8 * (r / 4) + 4 * gg + r % 4);
+      if (j <= see && !__builtin_isfinite(v)) o[db][r] += w * v;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// A lane's half of a row, O^T accumulators: O / l in bf16, or the split's sums.
+__device__ inline void put_row(const AttendArgs &p, int kvh, int row, int head, int tok, int sp, int gg, float m, float l, const f32x16 (&o)[4]) {
+  if (p.S > 1) {
+    const size_t slot = ((size_t)kvh * p.rows + row) * p.S + sp;
+    if (gg == 0) p.ml[slot] = make_float2(m, l);
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(float4 *)(p.part + slot * kHeadDim + 32 * db + 2 * r + 4 * gg) = make_float4(o[db][r], o[db][r + 1], o[db][r + 2], o[db][r + 3]);
+  } else {
+    const float inv = 1.f / l;
+    uint16_t *out = p.O + (size_t)head * p.o_hs + (size_t)tok * p.o_rs;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const bf16x2 a = {(__bf16)(o[db][r] * inv), (__bf16)(o[db][r + 1] * inv)};
+        const bf16x2 b = {(__bf16)(o[db][r + 2] * inv), (__bf16)(o[db][r + 3] * inv)};
+        *(uint2 *)(out + 32 * db + 2 * r + 4 * gg) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+      }
+  }
+}
+
+#define SA_KFRAG(tile, hf, ks) \
+  (*(const bf16x8 *)((const char *)(tile) + ((kbase ^ (unsigned)((2 * (ks) + gg) << 4)) + (hf) * 32 * 256)))
+#define SA_VTR(tile, db, key0) \
+  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6)) + (key0) * 256)))
+
+// A tile's scores (lane = row, accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4 of HF * 32) into a row's running
+// softmax and its outputs.  masked: keys from place lim + 1 (less 4gg) on are not seen.
+template <int HF>
+__device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, const uint16_t *Vt, unsigned vbase, float c,
+                                   float &m_run, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  if (masked) {
+#pragma unroll
+    for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (32 * hf + 8 * (r / 4) + r % 4 > lim) sacc[hf][r] = -INFINITY;
+  }
+  __builtin_amdgcn_s_setprio(0);
+  float tmax = -INFINITY;
+#pragma unroll
+  for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[hf][r]);
+  // The reference moves only when some row's maximum grew by more than 2^8: until then probabilities may exceed 1
+  // (by at most 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
+  if (__any(__builtin_fmaf(tmax, c, -m_run) > 8.f)) {
+    const float m_new = fmaxf(m_run, max_pair(tmax) * c);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - ((m_new == -INFINITY) ? 0.f : m_new));
+    m_run = m_new;
+    lacc[0] *= alpha;
+    lacc[1] *= alpha;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+  }
+  const float m_ref = (m_run == -INFINITY) ? 0.f : m_run;
+  // probabilities, a pair at a time, beside the products: see the sparse prefill for the order
+  auto soft2 = [&](int g, int j) {
+#pragma unroll
+    for (int e = 2 * j; e < 2 * j + 2; ++e)
+      sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[g >> 1][8 * (g & 1) + e], c, -m_ref));
+  };
+  u32x4 pbuf[2];
+  auto cvt2 = [&](int g, int j) {
+    const bf16x2 pr = {(__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j], (__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j + 1]};
+    pbuf[g & 1][j] = __builtin_bit_cast(uint32_t, pr);
+  };
+  // The normaliser sums the probabilities as rounded to bf16, so that a row stays a convex combination of its V rows;
+  // 4x4x4 products with ones do it on the matrix pipe.
+  const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+  s16x4 vlo[4], vhi[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) soft2(0, j);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    vlo[i] = SA_VTR(Vt, i & 3, 0);
+    vhi[i] = SA_VTR(Vt, i & 3, 8);
+  }
+#pragma unroll
+  for (int j = 0; j < 3; ++j) cvt2(0, j);
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int i = 0; i < 8 * HF; ++i) {
+    const int g = i >> 2, db = i & 3;
+    if (db == 0) {
+      cvt2(g, 3);
+      asm("" : "+v"(pbuf[g & 1]));
+    }
+    const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1]);
+    const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
+    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
+    const s16x8 ps = __builtin_bit_cast(s16x8, pb);
+    if (db == 0)
+      lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+    if (db == 3)
+      lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+    if (i + 4 < 8 * HF) {
+      vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
+      vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
+    }
+    if (g + 1 < 2 * HF) {
+      soft2(g + 1, db);
+      if (db > 0) cvt2(g + 1, db - 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// Few rows: one set of up to 32 query rows, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers on
+// the way.  K and V become bf16 on their way into LDS, from registers that were read a tile ahead.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
+  constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
+  constexpr int NC = KT * 8 / 64;             // 16-byte pieces of codes of K, and of V, that a lane stages per tile
+  constexpr int kMasked = 2;                  // tiles that some rows see and others do not, at most: 31 keys
+  __shared__ __attribute__((aligned(16))) uint16_t lds[WK][2][KT * 128];
   __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles whose V has an infinity or NaN
   __shared__ float s_m[4][32], s_l[4][32];
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int grp = WQ == 4 ? 0 : wave, wq = WQ == 4 ? wave : 0, gt = WQ == 4 ? tid : lane;
-
-  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then
-  // row tiles from the last one (the most keys) down.
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, rt = p.tiles - 1 - rest / p.S;
-  const int r0 = rt * 32 * WQ, r_last = min(r0 + 32 * WQ, p.rows) - 1;
-  const int seen_all = p.pos + r0 / p.g;                           // last key that every row of the workgroup sees
-  const int t_masked = (seen_all + 1) / KT;                        // first tile that some do not
-  const int n_tiles = (p.pos + r_last / p.g) / KT + 1;          // tiles that some row sees
+  // KV heads side by side, then splits; a single row tile
+  const int kvh = blockIdx.x % p.Hkv, sp = blockIdx.x / p.Hkv;
+  const int t_masked = (p.pos + 1) / KT;  // first tile that some rows do not see
+  const int n_tiles = (p.tokens - 1) / KT + 1;
   const int per = (n_tiles + p.S - 1) / p.S;
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
   const int n_closed = p.closed / KT;
 
-  // this lane's row, and the last keys that it, its wave's first and its wave's last row see
-  const int wr0 = min(r0 + 32 * wq, p.rows - 1), wr1 = min(r0 + 32 * wq + 31, p.rows - 1);
-  const int row = min(r0 + 32 * wq + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g);
-  const int see = p.pos + tok, see0 = p.pos + wr0 / p.g, see1 = p.pos + wr1 / p.g;
+  // this lane's row, and the last key that it sees
+  const int row = min(q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim;
   const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim;
@@ -143,11 +275,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs p) {
   float ksc = 1.f, vsc = 1.f;
   auto fetch = [&](int t) {
     if (t < n_closed) {
-      const size_t at = (size_t)t * KT * kHeadDim + gt * 16;
+      const size_t at = (size_t)t * KT * kHeadDim + lane * 16;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        kc[i] = *(const uint4 *)(Kh + at + (size_t)i * GT * 16);
-        vc[i] = *(const uint4 *)(Vh + at + (size_t)i * GT * 16);
+        kc[i] = *(const uint4 *)(Kh + at + (size_t)i * 1024);
+        vc[i] = *(const uint4 *)(Vh + at + (size_t)i * 1024);
       }
       const int blk = (t * KT) >> p.shift;
       ksc = ksh[blk];
@@ -156,17 +288,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs p) {
   };
   // LDS tiles are KT rows x 256 B, the 16-byte chunks of a row XOR-swizzled: K chunk c of row r at c ^ (r & 15) (b128
   // reads of 16 rows hit 64 banks), V chunk c at c ^ ((r & 3) << 2) (the transposing b64 reads do).
-  auto put_row = [&](uint16_t *tile, int r, int c16, int swz, const uint4 &lo, const uint4 &hi) {
+  auto put_keys = [&](uint16_t *tile, int r, int c16, int swz, const uint4 &lo, const uint4 &hi) {
     char *at = (char *)tile + r * 256;
     *(uint4 *)(at + (((2 * c16) ^ swz) << 4)) = lo;
     *(uint4 *)(at + (((2 * c16 + 1) ^ swz) << 4)) = hi;
   };
-  auto stage = [&](int t, int buf) {
+  auto stage = [&](int t) {
     const int j0 = t * KT;
     const bool masked = t >= t_masked;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int id = gt + i * GT, r = id >> 3, c16 = id & 7;
+      const int id = lane + 64 * i, r = id >> 3, c16 = id & 7;
       uint4 klo, khi, vlo, vhi;
       if (t < n_closed) {
         decode16<TYPE>(kc[i], ksc, klo, khi);
@@ -191,269 +323,413 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs p) {
         vlo = make_uint4(finite_only(vlo.x), finite_only(vlo.y), finite_only(vlo.z), finite_only(vlo.w));
         vhi = make_uint4(finite_only(vhi.x), finite_only(vhi.y), finite_only(vhi.z), finite_only(vhi.w));
       }
-      put_row(lds[grp][buf][0], r, c16, r & 15, klo, khi);
-      put_row(lds[grp][buf][1], r, c16, (r & 3) << 2, vlo, vhi);
+      put_keys(lds[wave][0], r, c16, r & 15, klo, khi);
+      put_keys(lds[wave][1], r, c16, (r & 3) << 2, vlo, vhi);
     }
   };
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
   const unsigned kbase = (unsigned)(q * 256) | (unsigned)((q & 15) << 4);
   unsigned vbase;
   {
     const int r = lane & 15, part = (lane >> 4) & 1, vrow = 4 * gg + (r >> 2);
     vbase = (unsigned)(vrow * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vrow & 3) << 2)) << 4) | (unsigned)((r & 1) << 3);
   }
-#define SA_KFRAG(tile, hf, ks) \
-  (*(const bf16x8 *)((const char *)(tile) + ((kbase ^ (unsigned)((2 * (ks) + gg) << 4)) + (hf) * 32 * 256)))
-#define SA_VTR(tile, db, key0) \
-  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6)) + (key0) * 256)))
 
-  auto attend = [&](int t, int buf) {
+  auto attend = [&](int t) {
     const int j0 = t * KT;
-    if (j0 > see1) return;
-    const bool needmask = j0 + KT - 1 > see0;
-    const int lim = see - j0 - 4 * gg;  // slot c of this lane is kept iff c <= lim
-    const uint16_t *Kt = lds[grp][buf][0], *Vt = lds[grp][buf][1];
-    // ---- S^T = K Q^T: lane = query row (q), accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4
-    f32x16 sacc[HF];
+    const uint16_t *Kt = lds[wave][0];
+    f32x16 sacc[1];  // S^T = K Q^T
+    bf16x8 kf[4];
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
+    for (int i = 0; i < 4; ++i) kf[i] = SA_KFRAG(Kt, 0, i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[hf][r] = 0.f;
-    {
-      bf16x8 kf[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) kf[i] = SA_KFRAG(Kt, i % HF, i / HF);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < 8 * HF; ++i) {
-        const int hf = i % HF, ks = i / HF;
-        sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[ks], sacc[hf], 0, 0, 0);
-        if (i + 4 < 8 * HF) kf[i & 3] = SA_KFRAG(Kt, (i + 4) % HF, (i + 4) / HF);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    if (needmask) {
-#pragma unroll
-      for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int c = 32 * hf + 8 * (r / 4) + (r % 4);
-          if (c > lim) sacc[hf][r] = -INFINITY;
-        }
-    }
-    __builtin_amdgcn_s_setprio(0);
-    float tmax = -INFINITY;
-#pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[hf][r]);
-    tmax = max_pair(tmax);
-    const float m_new = fmaxf(m_run, tmax * p.c);
-    // The reference moves only when some row's maximum grew by more than 2^8: until then probabilities may exceed 1
-    // (by at most 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
-    if (__any(m_new - m_run > 8.f)) {
-      const float alpha = __builtin_amdgcn_exp2f(m_run - ((m_new == -INFINITY) ? 0.f : m_new));
-      m_run = m_new;
-      lacc[0] *= alpha;
-      lacc[1] *= alpha;
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
-    }
-    const float m_ref = (m_run == -INFINITY) ? 0.f : m_run;
-    // ---- probabilities, a pair at a time, beside the products: see the sparse prefill for the order -----------
-    auto soft2 = [&](int g, int j) {
-#pragma unroll
-      for (int e = 2 * j; e < 2 * j + 2; ++e)
-        sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[g >> 1][8 * (g & 1) + e], p.c, -m_ref));
-    };
-    u32x4 pbuf[2];
-    auto cvt2 = [&](int g, int j) {
-      const bf16x2 pr = {(__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j], (__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j + 1]};
-      pbuf[g & 1][j] = __builtin_bit_cast(uint32_t, pr);
-    };
-    // The normaliser sums the probabilities as rounded to bf16, so that a row stays a convex combination of its V rows;
-    // 4x4x4 products with ones do it on the matrix pipe.
-    const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
-    constexpr int kProducts = 8 * HF;  // HF * 2 key steps x 4 d blocks
-    s16x4 vlo[4], vhi[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) soft2(0, j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      vlo[i] = SA_VTR(Vt, i & 3, 16 * (i >> 2));
-      vhi[i] = SA_VTR(Vt, i & 3, 16 * (i >> 2) + 8);
-    }
-#pragma unroll
-    for (int j = 0; j < 3; ++j) cvt2(0, j);
-    __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int i = 0; i < kProducts; ++i) {
-      const int g = i >> 2, db = i & 3;
-      if (db == 0) {
-        cvt2(g, 3);
-        asm("" : "+v"(pbuf[g & 1]));
-      }
-      const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1]);
-      const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
-      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
-      const s16x8 ps = __builtin_bit_cast(s16x8, pb);
-      if (db == 0)
-        lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
-      if (db == 3)
-        lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
-      if (i + 4 < kProducts) {
-        vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
-        vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
-      }
-      if (g + 1 < 2 * HF) {
-        soft2(g + 1, db);
-        if (db > 0) cvt2(g + 1, db - 1);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const f32x16 zero = {};
+      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
+      if (i + 4 < 8) kf[i & 3] = SA_KFRAG(Kt, 0, i + 4);
       __builtin_amdgcn_sched_barrier(0);
     }
+    absorb_tile(sacc, j0 + KT - 1 > p.pos, see - j0 - 4 * gg, lds[wave][1], vbase, p.c, m_run, lacc, oacc);
   };
 
-  if constexpr (WQ == 4) {
-    if (t_begin < t_end) {
-      fetch(t_begin);
-      stage(t_begin, 0);
-      if (t_begin + 1 < t_end) fetch(t_begin + 1);
-      for (int t = t_begin; t < t_end; ++t) {
-        const int cur = (t - t_begin) & 1;
-        __syncthreads();  // tile t is in LDS, and every wave is done with tile t - 1
-        if (t + 1 < t_end) stage(t + 1, cur ^ 1);
-        if (t + 2 < t_end) fetch(t + 2);
-        attend(t, cur);
-      }
-    }
-  } else {
-    if (t_begin + grp < t_end) fetch(t_begin + grp);
-    for (int t = t_begin + grp; t < t_end; t += WK) {
-      stage(t, 0);
-      wave_lds_sync();
-      if (t + WK < t_end) fetch(t + WK);
-      attend(t, 0);
-      wave_lds_sync();
-    }
+  if (t_begin + wave < t_end) fetch(t_begin + wave);
+  for (int t = t_begin + wave; t < t_end; t += WK) {
+    stage(t);
+    wave_lds_sync();
+    if (t + WK < t_end) fetch(t + WK);
+    attend(t);
+    wave_lds_sync();
   }
   // Non-finite values of V in tiles that only some rows see: their share, for the rows that do.  Seldom there, so the
   // scores are taken once more, plainly.
   if (t_end > t_masked) {
     __syncthreads();
-    const int base = max(t_begin, t_masked) * KT;
-    for (int j = base; j < t_end * KT; ++j) {
-      if (!__builtin_amdgcn_readfirstlane(rowbad[j - t_masked * KT]) || j >= p.tokens) continue;
-      if (WQ == 1 && (j / KT - t_begin) % WK != grp) continue;  // another wave's tile
-      float s = 0.f;
-      for (int d = 0; d < kHeadDim; ++d)
-        s = __builtin_fmaf(value(p.Q[(size_t)head * p.q_hs + (size_t)tok * p.q_rs + d]), element<TYPE>(p, kvh, p.K, p.k_scale, p.k_open, j, d), s);
-      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, p.c, m_run == -INFINITY ? 0.f : -m_run));
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float v = element<TYPE>(p, kvh, p.V, p.v_scale, p.v_open, j, 32 * db + 8 * (r / 4) + 4 * gg + r % 4);
-          if (j <= see && !__builtin_isfinite(v)) oacc[db][r] += w * v;
-          __builtin_amdgcn_sched_barrier(0);
-        }
+    for (int t = max(t_begin, t_masked); t < t_end; ++t) {
+      if ((t - t_begin) % WK != wave) continue;  // another wave's tile
+      for (uint64_t bad = __ballot(lane < KT && rowbad[(t - t_masked) * KT + (lane & (KT - 1))] != 0); bad != 0ull; bad &= bad - 1ull)
+        add_nonfinite<TYPE>(p, kvh, t * KT + __ffsll((unsigned long long)bad) - 1, head, tok, see, gg, m_run, oacc);
     }
   }
   const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
 
   // ---- out: O / l in bf16, or the split's sums ------------------------------------------------------
-  if constexpr (WQ == 4) {
-    const bool mine = r0 + 32 * wq + q < p.rows;
-    const size_t slot = ((size_t)kvh * p.rows + row) * p.S + sp;
-    if (mine && p.S > 1) {
-      if (gg == 0) p.ml[slot] = make_float2(m_run, l_run);
+  // the four waves' sums of the same rows, through the LDS of the tiles
+  float *const so = (float *)&lds[0][0][0];  // [4][32][128]
+  static_assert(sizeof(lds) >= 4 * 32 * 128 * 4, "holds the waves' outputs");
+  __syncthreads();
+  if (gg == 0) { s_m[wave][q] = m_run; s_l[wave][q] = l_run; }
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
+  for (int db = 0; db < 4; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *(float4 *)(p.part + slot * kHeadDim + 32 * db + 2 * r + 4 * gg) =
-              make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
-    } else if (mine) {
-      const float inv = 1.f / l_run;
-      uint16_t *o = p.O + (size_t)head * p.o_hs + (size_t)tok * p.o_rs;
+    for (int r = 0; r < 16; r += 4)
+      *(float4 *)(so + (wave * 32 + q) * kHeadDim + ((32 * db + 2 * r + 4 * gg) ^ ((q & 7) << 2))) =
+          make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
+  __syncthreads();
+  const int mr = tid >> 3, d0 = (tid & 7) * 16;  // 16 outputs of a row each
+  const int orow = mr;
+  if (orow < p.rows) {
+    float M = -INFINITY, L = 0.f, w[4];
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
+    for (int k = 0; k < 4; ++k) M = fmaxf(M, s_m[k][mr]);
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const bf16x2 a = {(__bf16)(oacc[db][r] * inv), (__bf16)(oacc[db][r + 1] * inv)};
-          const bf16x2 b = {(__bf16)(oacc[db][r + 2] * inv), (__bf16)(oacc[db][r + 3] * inv)};
-          *(uint2 *)(o + 32 * db + 2 * r + 4 * gg) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
-        }
+    for (int k = 0; k < 4; ++k) {
+      w[k] = s_m[k][mr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][mr] - M);
+      L += s_l[k][mr] * w[k];
     }
-  } else {
-    // the four waves' sums of the same rows, through the LDS of the tiles
-    float *const so = (float *)&lds[0][0][0][0];  // [4][32][128]
-    static_assert(sizeof(lds) >= 4 * 32 * 128 * 4, "holds the waves' outputs");
-    __syncthreads();
-    if (gg == 0) { s_m[wave][q] = m_run; s_l[wave][q] = l_run; }
+    const size_t slot = ((size_t)kvh * p.rows + orow) * p.S + sp;
+    const float inv = p.S > 1 ? 1.f : 1.f / L;
+    const int otok = orow / p.g;
+    uint16_t *o = p.O + (size_t)(kvh * p.g + orow - otok * p.g) * p.o_hs + (size_t)otok * p.o_rs;
+    if (p.S > 1 && d0 == 0) p.ml[slot] = make_float2(M, L);
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *(float4 *)(so + (wave * 32 + q) * kHeadDim + ((32 * db + 2 * r + 4 * gg) ^ ((q & 7) << 2))) =
-            make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
-    __syncthreads();
-    const int mr = tid >> 3, d0 = (tid & 7) * 16;  // 16 outputs of a row each
-    const int orow = r0 + mr;
-    if (orow < p.rows) {
-      float M = -INFINITY, L = 0.f, w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) M = fmaxf(M, s_m[k][mr]);
+    for (int i = 0; i < 16; i += 4) {
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        w[k] = s_m[k][mr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][mr] - M);
-        L += s_l[k][mr] * w[k];
+        const float4 x = *(const float4 *)(so + (k * 32 + mr) * kHeadDim + ((d0 + i) ^ ((mr & 7) << 2)));
+        a.x = __builtin_fmaf(x.x, w[k], a.x); a.y = __builtin_fmaf(x.y, w[k], a.y);
+        a.z = __builtin_fmaf(x.z, w[k], a.z); a.w = __builtin_fmaf(x.w, w[k], a.w);
       }
-      const size_t slot = ((size_t)kvh * p.rows + orow) * p.S + sp;
-      const float inv = p.S > 1 ? 1.f : 1.f / L;
-      const int otok = orow / p.g;
-      uint16_t *o = p.O + (size_t)(kvh * p.g + orow - otok * p.g) * p.o_hs + (size_t)otok * p.o_rs;
-      if (p.S > 1 && d0 == 0) p.ml[slot] = make_float2(M, L);
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4 x = *(const float4 *)(so + (k * 32 + mr) * kHeadDim + ((d0 + i) ^ ((mr & 7) << 2)));
-          a.x = __builtin_fmaf(x.x, w[k], a.x); a.y = __builtin_fmaf(x.y, w[k], a.y);
-          a.z = __builtin_fmaf(x.z, w[k], a.z); a.w = __builtin_fmaf(x.w, w[k], a.w);
-        }
-        if (p.S > 1) {
-          *(float4 *)(p.part + slot * kHeadDim + d0 + i) = a;
-        } else {
-          const bf16x2 u = {(__bf16)(a.x * inv), (__bf16)(a.y * inv)}, v = {(__bf16)(a.z * inv), (__bf16)(a.w * inv)};
-          *(uint2 *)(o + d0 + i) = make_uint2(__builtin_bit_cast(uint32_t, u), __builtin_bit_cast(uint32_t, v));
-        }
+      if (p.S > 1) {
+        *(float4 *)(p.part + slot * kHeadDim + d0 + i) = a;
+      } else {
+        const bf16x2 u = {(__bf16)(a.x * inv), (__bf16)(a.y * inv)}, v = {(__bf16)(a.z * inv), (__bf16)(a.w * inv)};
+        *(uint2 *)(o + d0 + i) = make_uint2(__builtin_bit_cast(uint32_t, u), __builtin_bit_cast(uint32_t, v));
       }
     }
   }
 }
 
-// The splits of a row joined: a wave per row, two outputs a lane.
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);  // KV head, row
-  if (at >= (int64_t)p.Hkv * p.rows) return;
-  const float2 ml = lane < p.S ? p.ml[at * p.S + lane] : make_float2(-INFINITY, 0.f);
-  float M = ml.x;
-  for (int e = 32; e >= 1; e >>= 1) M = fmaxf(M, __shfl_xor(M, e));
-  const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-  float L = ml.y * w;
-  for (int e = 32; e >= 1; e >>= 1) L += __shfl_xor(L, e);
-  float2 o = make_float2(0.f, 0.f);
-  for (int s = 0; s < p.S; ++s) {
-    const float ws = __shfl(w, s);
-    const float2 x = *(const float2 *)(p.part + (at * p.S + s) * kHeadDim + 2 * lane);
-    o.x = __builtin_fmaf(x.x, ws, o.x);
-    o.y = __builtin_fmaf(x.y, ws, o.y);
+// Many rows: four waves of 32 query rows each, which share tiles of 64 keys.
+//   K stays in codes: they go from memory into LDS as they are (the LDS DMA, no registers) and into the 8-bit matrix
+//   instructions, at twice the rate of the bf16 ones.  Q, in bf16, is cut into two codes of e4m3, q = hi + lo: hi is q
+//   rounded to 4 significant bits, and what is left fits 4 more, exactly, so that two products at twice the rate
+//   multiply all of q (an element below 2^-14 of its row's largest loses bits that are below 2^-23 of that one).  The scales of
+//   Q's rows and of the block of K are exponents that the instruction takes.
+//   V has to be multiplied with probabilities, which need bf16: its codes are turned into bf16 on their way into LDS, from
+//   registers that were read a tile ahead.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) {
+  constexpr int KT = 64, T = kThreads, NC = KT * 8 / T;  // NC: 16-byte pieces of K, and of V, that a thread moves per tile
+  constexpr int kMasked = 3;                             // tiles that some rows see and others do not, at most: 127 keys
+  // K of two tiles as codes, or of one in bf16 (open block); V of two tiles in bf16
+  __shared__ __attribute__((aligned(16))) uint8_t Ks[2][KT * 128];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[2][KT * 128];
+  __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles whose V has an infinity or NaN
+
+  const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then
+  // row tiles from the last one (the most keys) down.
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, rt = p.tiles - 1 - rest / p.S;
+  const int r0 = rt * kRowsMany, r_last = min(r0 + kRowsMany, p.rows) - 1;
+  const int seen_all = p.pos + r0 / p.g;                 // last key that every row of the workgroup sees
+  const int t_masked = (seen_all + 1) / KT;              // first tile that some do not
+  const int n_tiles = (p.pos + r_last / p.g) / KT + 1;   // tiles that some row sees
+  const int per = (n_tiles + p.S - 1) / p.S;
+  const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
+  const int n_closed = p.closed / KT, t_full = min(t_end, n_closed);  // tiles t_begin .. t_full - 1 are codes
+
+  // this lane's row, and the last keys that it, its wave's first and its wave's last row see
+  const int wr0 = min(r0 + 32 * wave, p.rows - 1), wr1 = min(r0 + 32 * wave + 31, p.rows - 1);
+  const int row = min(r0 + 32 * wave + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g);
+  const int see = p.pos + tok, see0 = p.pos + wr0 / p.g, see1 = p.pos + wr1 / p.g;
+
+  const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim;
+  const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim;
+  const float *ksh = p.k_scale + (size_t)kvh * (p.capacity >> p.shift), *vsh = p.v_scale + (size_t)kvh * (p.capacity >> p.shift);
+
+  // ---- K: 64 rows of 128 bytes, the 16-byte chunks of row r XOR-swizzled by r / 2 (the swizzle is applied on the global
+  // side: the lane that owns chunk c of row r reads chunk c ^ (r / 2) % 8), so that b128 reads of 8 rows hit 64 banks.
+  const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + wave * 1024;
+  const unsigned kvoff = (unsigned)((8 * wave + (lane >> 3)) * 128 + (((lane & 7) ^ ((lane >> 4) | (wave & 1) << 2)) << 4));
+  auto issue_k = [&](int t, int buf) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const uint8_t *src = Kh + ((size_t)t * KT + 32 * i) * kHeadDim;
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(kvoff), "s"(src),
+                   "s"(ldsK + (unsigned)(buf * KT * 128 + i * T * 16)) : "memory");
+    }
+  };
+  // ---- V: a thread's pieces of 16 codes, row vrow + 32 i
+  uint4 vc[NC];
+  const int vrow = tid >> 3, vch = tid & 7;
+  auto fetch_v = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) vc[i] = *(const uint4 *)(Vh + (size_t)t * KT * kHeadDim + tid * 16 + i * T * 16);
+  };
+  auto put_v = [&](int buf, int i, const uint4 &lo, const uint4 &hi) {
+    char *at = (char *)&Vs[buf][0] + (vrow + 32 * i) * 256;
+    const int swz = (vrow & 3) << 2;
+    *(uint4 *)(at + (((2 * vch) ^ swz) << 4)) = lo;
+    *(uint4 *)(at + (((2 * vch + 1) ^ swz) << 4)) = hi;
+  };
+  // Non-finite values of V in a tile that only some rows see: a row that does not gives them weight 0, and 0 x inf is not
+  // 0.  They stay out of the products and come back at the end for the rows that do.
+  auto mark = [&](int t, int i, bool bad) {
+    const uint64_t who = __ballot(bad);
+    if (vch == 0) rowbad[(t - t_masked) * KT + vrow + 32 * i] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
+  };
+  auto screen = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      mark(t, i, (nonfinite_codes<TYPE>(vc[i].x) | nonfinite_codes<TYPE>(vc[i].y) | nonfinite_codes<TYPE>(vc[i].z) | nonfinite_codes<TYPE>(vc[i].w)) != 0u);
+      vc[i] = make_uint4(finite_codes<TYPE>(vc[i].x), finite_codes<TYPE>(vc[i].y), finite_codes<TYPE>(vc[i].z), finite_codes<TYPE>(vc[i].w));
+    }
+  };
+
+  const bool open = t_end > max(t_begin, n_closed);  // has tiles of the open block, which come first
+  if (t_begin < t_full) {  // on their way while Q is read and cut
+    fetch_v(t_begin);
+    if (!open) issue_k(t_begin, 0);
   }
-  const int kvh = (int)(at / p.rows), row = (int)(at - (int64_t)kvh * p.rows), tok = row / p.g;
+  bf16x8 qf[8];  // Q^T fragments: B operand of the bf16 products, lane = row, 8 consecutive d per k-step half
+  {
+    const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 16 * ks + 8 * gg);
+  }
+  f32x16 oacc[4];
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+  float m_run = -INFINITY;
+  f32x4 lacc[2] = {};
+  unsigned vbase;
+  {
+    const int r = lane & 15, part = (lane >> 4) & 1, vr = 4 * gg + (r >> 2);
+    vbase = (unsigned)(vr * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vr & 3) << 2)) << 4) | (unsigned)((r & 1) << 3);
+  }
+
+  // ---- the open block first: its one or two tiles are bf16, their products too -----------------------------
+  for (int t = max(t_begin, n_closed); t < t_end; ++t) {
+    const int j0 = t * KT;
+    uint16_t *const Kt = (uint16_t *)&Ks[0][0];  // both buffers
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int r = vrow + 32 * i, j = j0 + r;
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (j < p.tokens) {  // zeros behind the tokens
+        const size_t at = (((size_t)kvh << p.shift) + (j - p.closed)) * kHeadDim + vch * 16;
+        x[0] = *(const uint4 *)(p.k_open + at);
+        x[1] = *(const uint4 *)(p.k_open + at + 8);
+        x[2] = *(const uint4 *)(p.v_open + at);
+        x[3] = *(const uint4 *)(p.v_open + at + 8);
+      }
+      if (t >= t_masked) {
+        uint32_t bad = 0u;
+#pragma unroll
+        for (int k = 2; k < 4; ++k) {
+          bad |= nonfinite(x[k].x) | nonfinite(x[k].y) | nonfinite(x[k].z) | nonfinite(x[k].w);
+          x[k] = make_uint4(finite_only(x[k].x), finite_only(x[k].y), finite_only(x[k].z), finite_only(x[k].w));
+        }
+        mark(t, i, bad != 0u);
+      }
+      char *at = (char *)Kt + r * 256;  // chunk c of row r at c ^ (r & 15)
+      *(uint4 *)(at + (((2 * vch) ^ (r & 15)) << 4)) = x[0];
+      *(uint4 *)(at + (((2 * vch + 1) ^ (r & 15)) << 4)) = x[1];
+      put_v(1, i, x[2], x[3]);
+    }
+    __syncthreads();
+    if (j0 <= see1) {
+      f32x16 sacc[2] = {};
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const bf16x8 kf = *(const bf16x8 *)((const char *)Kt + (32 * hf + q) * 256 + (((2 * ks + gg) ^ (q & 15)) << 4));
+          sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sacc[hf], 0, 0, 0);
+        }
+      absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[1], vbase, p.c, m_run, lacc, oacc);
+    }
+  }
+  if (open && t_begin < t_full) {
+    __syncthreads();
+    issue_k(t_begin, 0);
+  }
+
+  if (t_begin < t_full) {
+    // ---- Q in codes: scales 2^e (hi) and 2^(e - 4) (lo) of a row, the least e with every |q| <= 448 2^e
+    i32x8 qc[2][2];  // [64 d][hi, lo]: bytes d = 64 s + 32 gg ..
+    int qscale[2];
+    {
+      uint32_t top = 0;
+      const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
+      uint4 x[2][4];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[s][k] = *(const uint4 *)(qrow + 64 * s + 32 * gg + 8 * k);
+          const uint32_t w[4] = {x[s][k].x, x[s][k].y, x[s][k].z, x[s][k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+        }
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const int e = scale_exponent<SA_CACHE_E4M3>(min(top, 0x7F7Fu));
+      const float up = __uint_as_float((uint32_t)(127 - e) << 23);
+      qscale[0] = 127 + e;
+      qscale[1] = 127 + e - 4;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t w[4] = {x[s][k].x, x[s][k].y, x[s][k].z, x[s][k].w};
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const uint32_t hi = encode4<SA_CACHE_E4M3>(w[i], w[i + 1], up);
+            const f32_pair h0 = decode2f<SA_CACHE_E4M3, false>(hi), h1 = decode2f<SA_CACHE_E4M3, true>(hi);
+            const float l0 = (value((uint16_t)w[i]) * up - h0[0]) * 16.f, l1 = (value((uint16_t)(w[i] >> 16)) * up - h0[1]) * 16.f;
+            const float l2 = (value((uint16_t)w[i + 1]) * up - h1[0]) * 16.f, l3 = (value((uint16_t)(w[i + 1] >> 16)) * up - h1[1]) * 16.f;
+            int lo = __builtin_amdgcn_cvt_pk_fp8_f32(l0, l1, 0, false);
+            lo = __builtin_amdgcn_cvt_pk_fp8_f32(l2, l3, lo, true);
+            qc[s][0][2 * k + i / 2] = (int)hi;
+            qc[s][1][2 * k + i / 2] = lo;
+          }
+        }
+    }
+    const unsigned kbase = (unsigned)(q * 128) | (unsigned)((((2 * gg) ^ (q >> 1)) & 7) << 4);
+    constexpr int kType = TYPE == SA_CACHE_E4M3 ? 0 : 1;
+
+    float vsc = uniform_load(vsh, (t_begin * KT) >> p.shift);
+    auto convert_v = [&](int buf, int i) {
+      uint4 lo, hi;
+      decode16<TYPE>(vc[i], vsc, lo, hi);
+      put_v(buf, i, lo, hi);
+    };
+    if (t_begin >= t_masked) screen(t_begin);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) convert_v(0, i);
+    if (t_begin + 1 < t_full) {
+      fetch_v(t_begin + 1);
+      vsc = uniform_load(vsh, ((t_begin + 1) * KT) >> p.shift);
+    }
+    for (int t = t_begin; t < t_full; ++t) {
+      const int cur = (t - t_begin) & 1, j0 = t * KT;
+      // K of this tile has landed, and V of the next one; after the barrier both buffers of the tile hold it and
+      // every wave is done with the tile before
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+      __syncthreads();
+      const bool more = t + 1 < t_full;
+      if (more) {
+        issue_k(t + 1, cur ^ 1);
+        if (t + 1 >= t_masked) screen(t + 1);
+      }
+      // S^T = K Q^T, two products per fragment of K, the reads of the fragment after the next behind them; beside them V of
+      // the next tile becomes bf16 (what is left in the registers, behind the last tile: nobody reads it)
+      const int kscale = (int)(__float_as_uint(uniform_load(ksh, j0 >> p.shift)) >> 23);
+      const char *Kt = (const char *)&Ks[cur][0];
+      auto k_frag = [&](int f) {
+        const unsigned at = (kbase ^ (unsigned)((f >> 1) << 6)) + (f & 1) * 32 * 128;
+        return __builtin_shufflevector(*(const i32x4 *)(Kt + at), *(const i32x4 *)(Kt + (at ^ 16u)), 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      f32x16 sacc[2];
+      i32x8 kf[2];
+      uint4 vx[2];
+      kf[0] = k_frag(0);
+      kf[1] = k_frag(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int f = i >> 1, hf = f & 1, s = f >> 1, part = i & 1;
+        const f32x16 zero = {};
+        sacc[hf] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[f & 1], qc[s][part], s == 0 && part == 0 ? zero : sacc[hf], kType, 0, 0, kscale,
+                                                                  0, qscale[part]);
+        if (part == 1 && f + 2 < 4) kf[f & 1] = k_frag(f + 2);
+#pragma unroll
+        for (int w = NC * i; w < NC * (i + 1); ++w) {
+          const uint32_t code = w & 4 ? (w & 2 ? vc[w >> 3].w : vc[w >> 3].z) : (w & 2 ? vc[w >> 3].y : vc[w >> 3].x);
+          const uint32_t two = w & 1 ? decode2<TYPE, true>(code, vsc) : decode2<TYPE, false>(code, vsc);
+          uint4 &d = vx[(w >> 2) & 1];
+          ((w & 3) == 0 ? d.x : (w & 3) == 1 ? d.y : (w & 3) == 2 ? d.z : d.w) = two;
+          if ((w & 7) == 7) put_v(cur ^ 1, w >> 3, vx[0], vx[1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t + 2 < t_full) {
+        fetch_v(t + 2);
+        vsc = uniform_load(vsh, ((t + 2) * KT) >> p.shift);
+      }
+      if (j0 <= see1) absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[cur], vbase, p.c, m_run, lacc, oacc);
+    }
+  }
+
+  // ---- non-finite values of V in tiles that only some rows see
+  if (t_end > t_masked) {
+    __syncthreads();
+    for (int t = max(t_begin, t_masked); t < t_end; ++t)
+      for (uint64_t bad = __ballot(rowbad[(t - t_masked) * KT + lane] != 0); bad != 0ull; bad &= bad - 1ull)
+        add_nonfinite<TYPE>(p, kvh, t * KT + __ffsll((unsigned long long)bad) - 1, head, tok, see, gg, m_run, oacc);
+  }
+  const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
+  if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, row, head, tok, sp, gg, m_run, l_run, oacc);
+}
+
+// The splits of a row joined: WAVES waves per row, each every WAVES-th split, two outputs a lane, the reads of eight
+// splits in flight.  One wave and a split after the other took 19 us for 32 rows of 64 splits.
+template <int WAVES>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
+  __shared__ float2 part[kThreads / 64][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k0 = wave % WAVES;
+  const int all = p.Hkv * p.rows, at = min((int)blockIdx.x * (kThreads / 64 / WAVES) + wave / WAVES, all - 1);  // KV head, row
+  const float2 ml = lane < p.S ? p.ml[(size_t)at * p.S + lane] : make_float2(-INFINITY, 0.f);
+  const float *src = p.part + (size_t)at * p.S * kHeadDim + 2 * lane;
+  float2 o = make_float2(0.f, 0.f), x[8];
+  float w = 0.f, L = 0.f;
+  for (int s0 = k0; s0 < p.S; s0 += 8 * WAVES) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s0 + i * WAVES < p.S) x[i] = *(const float2 *)(src + (size_t)(s0 + i * WAVES) * kHeadDim);
+    if (s0 == k0) {  // once, with the first reads on their way
+      float M = ml.x;
+      for (int e = 32; e >= 1; e >>= 1) M = fmaxf(M, __shfl_xor(M, e));
+      w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+      L = ml.y * w;
+      for (int e = 32; e >= 1; e >>= 1) L += __shfl_xor(L, e);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s0 + i * WAVES < p.S) {
+        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s0 + i * WAVES));
+        o.x = __builtin_fmaf(x[i].x, ws, o.x);
+        o.y = __builtin_fmaf(x[i].y, ws, o.y);
+      }
+  }
+  if (WAVES > 1) {
+    part[wave][lane] = o;
+    __syncthreads();
+    if (k0 != 0) return;
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) {
+      o.x += part[wave + k][lane].x;
+      o.y += part[wave + k][lane].y;
+    }
+  }
+  const int kvh = at / p.rows, row = at - kvh * p.rows, tok = row / p.g;
   const bf16x2 r = {(__bf16)(o.x / L), (__bf16)(o.y / L)};
   *(uint32_t *)(p.O + (size_t)(kvh * p.g + row - tok * p.g) * p.o_hs + (size_t)tok * p.o_rs + 2 * lane) = __builtin_bit_cast(uint32_t, r);
 }
@@ -481,24 +757,26 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   const int per_wg = few ? kRowsFew : kRowsMany;
   a.tiles = (a.rows + per_wg - 1) / per_wg;
   // Splits of the keys: two workgroups a compute unit in all, 128 (few rows) or 256 keys a workgroup at least.
-  const int64_t wgs = (int64_t)a.tiles * sh.Hkv;
+  const int64_t wgs = (int64_t)a.tiles * sh.Hkv, least = few ? 128 : 256;
   int64_t S = 2 * (int64_t)sh.n_cu / wgs;
-  S = std::min<int64_t>(S, (a.tokens + (few ? 127 : 255)) / (few ? 128 : 256));
+  S = std::min<int64_t>(S, (a.tokens + least - 1) / least);
   S = std::min<int64_t>(S, (int64_t)(max_slots(sh) / ((size_t)a.rows * sh.Hkv)));
   a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
-  if (c.type == SA_CACHE_E4M3) {
-    if (few) attend_kernel<SA_CACHE_E4M3, 1><<<grid, kThreads, 0, st>>>(a);
-    else attend_kernel<SA_CACHE_E4M3, 4><<<grid, kThreads, 0, st>>>(a);
+  const bool e4m3 = c.type == SA_CACHE_E4M3;
+  if (few) {
+    if (e4m3) attend_few_kernel<SA_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
+    else attend_few_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
   } else {
-    if (few) attend_kernel<SA_CACHE_E5M2, 1><<<grid, kThreads, 0, st>>>(a);
-    else attend_kernel<SA_CACHE_E5M2, 4><<<grid, kThreads, 0, st>>>(a);
+    if (e4m3) attend_rows_kernel<SA_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
+    else attend_rows_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
   }
   if (a.S > 1) {
-    const int64_t all = (int64_t)sh.Hkv * a.rows;
-    join_kernel<<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+    const int all = sh.Hkv * a.rows;
+    if (a.S > 8) join_kernel<4><<<all, kThreads, 0, st>>>(a);
+    else join_kernel<1><<<(all + kThreads / 64 - 1) / (kThreads / 64), kThreads, 0, st>>>(a);
   }
   return hipGetLastError();
 }

@@ -52,4 +52,15 @@ __device__ inline f32_pair decode2f(uint32_t w) {
   else return __builtin_amdgcn_cvt_pk_f32_bf8((int)w, HALF);
 }
 
+// Bit 7 of every byte of a word of codes that is an infinity or NaN; and the word with 0 in their place.
+template <int TYPE>
+__device__ inline uint32_t nonfinite_codes(uint32_t w) {
+  return ((w & 0x7F7F7F7Fu) + (TYPE == SA_CACHE_E4M3 ? 0x01010101u : 0x04040404u)) & 0x80808080u;
+}
+template <int TYPE>
+__device__ inline uint32_t finite_codes(uint32_t w) {
+  const uint32_t bad = nonfinite_codes<TYPE>(w);
+  return w & ~((bad << 1) - (bad >> 7));
+}
+
 }  // namespace sa
