@@ -6,7 +6,6 @@ another implementation.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 
@@ -307,7 +306,7 @@ class Rotary:
             pass
 
 
-_NOTHING = contextlib.nullcontext()
+_NO_ROWS = SaRows()
 _ROTARY_FIELDS = {name for name, _ in SaRotaryConfig._fields_}
 
 
@@ -326,23 +325,21 @@ class Cache:
         if d != 128 or capacity % block:
             raise SaError(1, "a cache holds rows of 128 elements and whole blocks")
         self.k, self.v, self.k_scale, self.v_scale, self.k_open, self.v_open = self.tensors
-        self.heads, self.capacity, self.block, self.type = heads, capacity, block, cache_type
+        self.heads, self.capacity, self.block, self.type, self.device = heads, capacity, block, cache_type, k.get_device()
         self._struct = SaCache(*[t.data_ptr() for t in self.tensors], capacity, cache_type)
 
     def struct(self):
         return self._struct
 
 
-def _rows(t, heads, device, what):
-    """A [heads, n, 128] bf16 tensor on GPU `device` as sa_rows; its last dimension adjacent, any order of the others."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != heads or shape[2] != 128 or stride[2] != 1 or t.element_size() != 2:
-        raise SaError(1, f"{what} must be a 16-bit tensor [{heads}, n, 128] with adjacent elements")
-    if t.get_device() != device:
-        raise SaError(1, f"{what} is not on the session's device {device}")
-    if stride[0] <= 0 and stride[1] <= 0 and shape[0] * shape[1] > 1:  # two zeros would stand for contiguous rows
-        raise SaError(1, f"{what} repeats one row")
-    return SaRows(t.data_ptr(), stride[0], stride[1])
+def _rows(t, shape, bf16, device, what):
+    """A bf16 tensor of `shape` [heads, n, 128] on GPU `device` as sa_rows; its last dimension adjacent, any order of the others."""
+    if t.shape != shape or t.dtype is not bf16 or t.get_device() != device:
+        raise SaError(1, f"{what} must be a bf16 tensor {list(shape)} on the session's device {device}, not {t.dtype} {list(t.shape)} on {t.device}")
+    heads, row, one = t.stride()
+    if one != 1 or (heads <= 0 and row <= 0 and shape[0] * shape[1] > 1):  # two zeros would stand for contiguous rows
+        raise SaError(1, f"{what} must have adjacent elements, and not one row for all")
+    return SaRows(t.data_ptr(), heads, row)
 
 
 class Session:
@@ -356,6 +353,9 @@ class Session:
         self.device = torch.device(device)
         self._known_index = None
         self._attend_scratch = None
+        self._get_device = torch._C._cuda_getDevice
+        self._bf16, self._hq, self._hkv, self._block = torch.bfloat16, n_q_heads, n_kv_heads, block
+        self._lib = library()
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
         cfg = SaConfig()
         cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim = n_q_heads, n_kv_heads, 128
@@ -385,6 +385,7 @@ class Session:
         self.blkcols = torch.empty((H, self.cap_b), dtype=i32, device=dev)
         assert [t.nbytes for t in self.index_tensors()] == ib
         self.ws = torch.empty(sa_workspace_bytes(self.ctx) + 256, dtype=torch.uint8, device=dev)
+        self._gpu = self.ws.get_device()
         off = (-self.ws.data_ptr()) % 256
         sa_set_workspace(self.ctx, self.ws.data_ptr() + off, self.ws.nbytes - off)
 
@@ -445,29 +446,32 @@ class Session:
         static device array (no workspace needed, nothing allocated)."""
         sa_sparse_decode_static(self.ctx, q, K, V, self._index(), pos, o, self.stream())
 
-    def _current(self, device):
-        """A context in which the session's device, which the library launches on, is the current one."""
-        return _NOTHING if self.torch.cuda.current_device() == device else self.torch.cuda.device(device)
-
     def rotate(self, rotary, Q, K, Q_out, K_out, pos=0, positions=None):
         """Rotary positions of Q [n_q_heads, n, 128] and K [n_kv_heads, n, 128] (either may be None), positions pos,
         pos + 1, ... or an int32 tensor of n; the outputs may be the inputs."""
-        device = self._device_index()
+        device, bf16 = self._gpu, self._bf16
+        if self._get_device() != device:  # the library launches on the current device
+            with self.torch.cuda.device(device):
+                return self.rotate(rotary, Q, K, Q_out, K_out, pos, positions)
         n = (K if Q is None else Q).shape[1]
-        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
-        rows = []
-        for x, y, heads in ((Q, Q_out, hq), (K, K_out, hkv)):
-            if x is None:
-                rows += [SaRows(), SaRows()]
-                continue
-            if x.shape[1] != n or y.shape[1] != n:
-                raise SaError(1, "Q, K and the outputs must have the same number of rows")
-            rows += [_rows(x, heads, device, "a tensor to rotate"), _rows(y, heads, device, "an output")]
-        if positions is not None and (positions.dtype != self.torch.int32 or tuple(positions.shape) != (n,) or
-                                      not positions.is_contiguous() or positions.get_device() != device):
-            raise SaError(1, "positions must be a contiguous int32 tensor on the session's device, one per row")
-        with self._current(device):
-            sa_rotary_embed(self.ctx, rotary, rows[0], rows[2], n, pos, positions, rows[1], rows[3], self.stream())
+        q = qo = k = ko = _NO_ROWS
+        if Q is not None:
+            shape = (self._hq, n, 128)
+            q = _rows(Q, shape, bf16, device, "Q")
+            qo = q if Q_out is Q else _rows(Q_out, shape, bf16, device, "Q_out")
+        if K is not None:
+            shape = (self._hkv, n, 128)
+            k = _rows(K, shape, bf16, device, "K")
+            ko = k if K_out is K else _rows(K_out, shape, bf16, device, "K_out")
+        at = None
+        if positions is not None:
+            if (positions.dtype is not self.torch.int32 or positions.shape != (n,) or not positions.is_contiguous() or
+                    positions.get_device() != device):
+                raise SaError(1, "positions must be a contiguous int32 tensor on the session's device, one per row")
+            at = positions.data_ptr()
+        st = self._lib.sa_rotary_embed(self.ctx, rotary.handle, q, k, n, pos, at, qo, ko, self._raw_stream(device))
+        if st:
+            _check(st, self.ctx)
 
     def cache(self, capacity, cache_type=SA_CACHE_E4M3):
         """An empty 8-bit cache for `capacity` tokens (a multiple of block)."""
@@ -478,30 +482,37 @@ class Session:
         assert [x.nbytes for x in bufs] == sizes
         return Cache(*bufs, cache_type)
 
-    def _own_cache(self, cache):
-        if cache.heads != self.cfg.n_kv_heads or cache.block != self.cfg.block:
-            raise SaError(1, f"the cache has {cache.heads} heads and blocks of {cache.block}, the session {self.cfg.n_kv_heads} and {self.cfg.block}")
-        device = self._device_index()
-        if cache.k.get_device() != device:
-            raise SaError(1, f"the cache is not on the session's device {device}")
-        return device
+    def _own(self, cache):
+        """The cache's struct, if the cache fits the session."""
+        if cache.heads != self._hkv or cache.block != self._block or cache.device != self._gpu:
+            raise SaError(1, f"the cache has {cache.heads} heads and blocks of {cache.block} on device {cache.device}, "
+                             f"the session {self._hkv} and {self._block} on {self._gpu}")
+        return cache.struct()
 
     def append(self, cache, K, V, pos):
         """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds."""
-        if K.shape[1] != V.shape[1]:
-            raise SaError(1, "K and V must have the same number of rows")
-        h, device = self.cfg.n_kv_heads, self._own_cache(cache)
-        with self._current(device):
-            sa_cache_append(self.ctx, cache, _rows(K, h, device, "K"), _rows(V, h, device, "V"), K.shape[1], pos, self.stream())
+        device, struct = self._gpu, self._own(cache)
+        if self._get_device() != device:
+            with self.torch.cuda.device(device):
+                return self.append(cache, K, V, pos)
+        n = K.shape[1]
+        shape = (self._hkv, n, 128)
+        st = self._lib.sa_cache_append(self.ctx, struct, _rows(K, shape, self._bf16, device, "K"), _rows(V, shape, self._bf16, device, "V"),
+                                       n, pos, self._raw_stream(device))
+        if st:
+            _check(st, self.ctx)
 
     def decode_cached(self, cache, q, pos, o):
         """decode() with K and V out of a cache that holds tokens 0..pos."""
-        device, shape = self._own_cache(cache), (self.cfg.n_q_heads, 128)
+        device, struct = self._gpu, self._own(cache)
+        if self._get_device() != device:
+            with self.torch.cuda.device(device):
+                return self.decode_cached(cache, q, pos, o)
+        shape, bf16 = (self._hq, 128), self._bf16
         for t in (q, o):
-            if tuple(t.shape) != shape or t.element_size() != 2 or not t.is_contiguous() or t.get_device() != device:
-                raise SaError(1, f"q and o must be contiguous 16-bit tensors {shape} on the session's device")
-        with self._current(device):
-            sa_cache_decode(self.ctx, cache, q, self._index(), pos, o, self.stream())
+            if t.shape != shape or t.dtype is not bf16 or not t.is_contiguous() or t.get_device() != device:
+                raise SaError(1, f"q and o must be contiguous bf16 tensors {list(shape)} on the session's device")
+        sa_cache_decode(self.ctx, struct, q, self._index(), pos, o, self._raw_stream(device))
 
     def attend_scratch(self):
         """The session's scratch of attend(), allocated at the first use and kept."""
@@ -514,13 +525,18 @@ class Session:
 
     def attend(self, cache, Q, pos, O):
         """Causal attention of the newest tokens, Q and O [n_q_heads, n, 128], over a cache that holds pos + n."""
-        if Q.shape[1] != O.shape[1]:
-            raise SaError(1, "Q and O must have the same number of rows")
-        h, device = self.cfg.n_q_heads, self._own_cache(cache)
-        _, scratch, size = self.attend_scratch()
-        with self._current(device):
-            sa_cache_attend(self.ctx, cache, _rows(Q, h, device, "Q"), Q.shape[1], pos, _rows(O, h, device, "O"), scratch, size,
-                            self.stream())
+        device, struct = self._gpu, self._own(cache)
+        if self._get_device() != device:
+            with self.torch.cuda.device(device):
+                return self.attend(cache, Q, pos, O)
+        _, scratch, size = self._attend_scratch or self.attend_scratch()
+        n = Q.shape[1]
+        shape = (self._hq, n, 128)
+        q = _rows(Q, shape, self._bf16, device, "Q")
+        st = self._lib.sa_cache_attend(self.ctx, struct, q, n, pos, q if O is Q else _rows(O, shape, self._bf16, device, "O"), scratch, size,
+                                       self._raw_stream(device))
+        if st:
+            _check(st, self.ctx)
 
     def search_patterns(self, Q, K, V, target_pairs, eps_pairs):
         """Alg. 1 on the scores of the last estimate(): one dict per head."""

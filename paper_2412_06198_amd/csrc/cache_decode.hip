@@ -1,8 +1,8 @@
 // One decode step over the prefill index, K and V out of the 8-bit cache: the keys, their order and the launch are
-// those of the step on bf16 tensors (decode.hip), half the bytes.  A key is read by 8 lanes as one 128-byte row of
-// codes of K and one of V and the two scales of its block; a lane holds 16 elements.  s = scale_K (q . codes) and
-// p scale_V codes: the scales meet one number per key, not its elements.  The open block, at most 127 keys in bf16, is
-// one step of one workgroup of its own.
+// those of the step on bf16 tensors (decode.hip), half the bytes.  A key is read by 16 lanes as one 128-byte row
+// of codes of K and one of V and the two scales of its block.  s = scale_K (q . codes) and
+// p scale_V codes: the scales meet one number per key, not its elements.  The open block, at most 127 keys in bf16, has
+// a workgroup of its own.
 #include <algorithm>
 
 #include "cache_codes.h"
@@ -27,23 +27,22 @@ struct CacheDecArgs {
 };
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kLanes = 8, kSlots = 64 / kLanes;  // lanes of a key, keys that a wave reads at once
-constexpr int U = 4;                             // rows of K and of V that a lane has in flight per step
+constexpr int kLanes = 16, kSlots = 64 / kLanes;  // lanes of a key, keys that a wave reads at once
+// Rows of K and of V that a lane has in flight per step.  2: up to 0.4 us faster on short lists, up to 2 slower on long ones;
+// 8 lanes a key with 16 bytes each: 3 % faster at 32 heads and 128K tokens, 0.1 to 0.8 us slower elsewhere.
+constexpr int U = 4;
 constexpr int kStep = kSlots * U;
-constexpr int kRing = 128;                       // keys of a wave that are resolved and not yet read: 31 + 64 at most
-constexpr int kMinChunk = kWaves * kStep;        // keys of a workgroup: one step of each wave, or the open block
-static_assert(kMinChunk >= 127, "the open block is one step");
+constexpr int kRing = 128;                        // keys of a wave that are resolved and not yet read: 15 + 64 at most
+constexpr int kMinChunk = kWaves * kStep;         // keys of a workgroup: one step of each wave
 
-// Sum over the 8 lanes of a key, on each of them: partners at distance 7, 2 and 1.
-__device__ inline float sum8(float x) {
+// Sum over 16 lanes, on each of them: partners at distance 8, 7, 2 and 1.
+__device__ inline float sum16(float x) {
+  x += row_move<0x128>(x);
   x += row_move<0x141>(x);
   x += row_move<0x4E>(x);
   x += row_move<0xB1>(x);
   return x;
 }
-// A reduction over the eight slots of a wave, on each lane.
-template <typename F>
-__device__ inline float over_keys(float x, F f) { return over_slots(f(x, row_move<0x128>(x)), f); }
 
 // A head's key list, in this order: keys of the kept blocks, columns, diagonal keys, generated keys in full blocks; and
 // how it is shared out: workgroups 0 .. main - 1 take `chunk` keys each, the next one the open block if it has any.
@@ -70,7 +69,7 @@ __device__ inline KeyList key_list(const CacheDecArgs &p, int h) {
 
 // grid (S + 1, Hq), 256 threads.  Each wave walks a quarter of the workgroup's keys by itself: 64 lanes resolve 64
 // list places (which key, does it count here), the keys that count queue up in the wave's ring, and a step
-// reads the rows of 32 of them, slot s of 8 lanes every eighth one, lane ln elements 16 ln .. 16 ln + 15.
+// reads the rows of 16 of them, slot s of 16 lanes every fourth one, lane ln elements 8 ln .. 8 ln + 7.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) {
   __shared__ __attribute__((aligned(16))) uint32_t blkbm[kMaxSeq / 64 / 32];  // key blocks kept for the last row block
@@ -83,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
   const int sp = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, kvh = h / p.g;
   const int N = p.N, nb = p.nb, b = 1 << p.shift, shift = p.shift;
   const int lane = tid & 63, ln = tid & (kLanes - 1), slot = lane / kLanes, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint4 q0 = *(const uint4 *)(p.q + (size_t)h * kHeadDim + ln * 16), q1 = *(const uint4 *)(p.q + (size_t)h * kHeadDim + ln * 16 + 8);
+  const uint4 qx = *(const uint4 *)(p.q + (size_t)h * kHeadDim + ln * 8);
   const KeyList L = key_list(p, h);
   if (sp >= L.n) return;
   float *part = p.part + (size_t)h * gridDim.x * kPartStride;
@@ -92,27 +91,21 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
   uint64_t seen = 0;
   if (claims) seen = __hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 
-  float qv[16], m = -INFINITY, l = 0.f, acc[16];
-  {
-    float lo[8], hi[8];
-    unpack8(q0, lo);
-    unpack8(q1, hi);
+  float qv[8], m = -INFINITY, l = 0.f, acc[8];
+  unpack8(qx, qv);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { qv[e] = lo[e]; qv[8 + e] = hi[e]; }
-  }
-#pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  // The softmax step of U keys a slot, of which the first n of the wave's count: key(u, f) and val(u, f) give a
-  // row's 16 elements, sk and sv what they are multiplied with.
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  // The softmax step of U keys a slot, of which the first n of the wave's count: key(u, f) and val(u, f) give this lane's
+  // elements of a row, sk and sv what they are multiplied with.
   auto absorb = [&](auto key, auto val, const float (&sk)[U], const float (&sv)[U], int n) {
     float s[U], m_new = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float kf[16], dot = 0.f;
+      float kf[8], dot = 0.f;
       key(u, kf);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dot = __builtin_fmaf(kf[e], qv[e], dot);
-      s[u] = kSlots * u + slot < n ? sum8(dot) * (sk[u] * p.c) : -INFINITY;
+      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(kf[e], qv[e], dot);
+      s[u] = kSlots * u + slot < n ? sum16(dot) * (sk[u] * p.c) : -INFINITY;
       m_new = fmaxf(m_new, s[u]);
     }
     const float m_ref = m_new == -INFINITY ? 0.f : m_new;
@@ -120,48 +113,39 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
     m = m_new;
     l *= alpha;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] *= alpha;
+    for (int e = 0; e < 8; ++e) acc[e] *= alpha;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float pv = __builtin_amdgcn_exp2f(s[u] - m_ref), pw = pv * sv[u];
-      float vf[16];
+      float vf[8];
       val(u, vf);
       l += pv;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[e] = __builtin_fmaf(pw, vf[e], acc[e]);
+      for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(pw, vf[e], acc[e]);
     }
   };
 
   if (sp == L.main) {  // the open block
-    const size_t at = (size_t)kvh * b * kHeadDim + ln * 16;
-    uint4 kx[U][2], vx[U][2];
+    const size_t at = (size_t)kvh * b * kHeadDim + ln * 8;
     float one[U];
-    const int n = min(max(L.rest - wave * kStep, 0), kStep);
-    if (n > 0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) one[u] = 1.f;
+    for (int base = wave * kStep; base < L.rest; base += kWaves * kStep) {
+      uint4 kx[U], vx[U];
+      const int n = min(L.rest - base, kStep);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        one[u] = 1.f;
-        const size_t row = at + (size_t)(wave * kStep + min(kSlots * u + slot, n - 1)) * kHeadDim;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          kx[u][i] = *(const uint4 *)(p.k_open + row + 8 * i);
-          vx[u][i] = *(const uint4 *)(p.v_open + row + 8 * i);
-        }
+        const size_t row = at + (size_t)(base + min(kSlots * u + slot, n - 1)) * kHeadDim;
+        kx[u] = *(const uint4 *)(p.k_open + row);
+        vx[u] = *(const uint4 *)(p.v_open + row);
       }
-      if (claims) claim(arrived, seen, p.token);
+      if (claims && base == wave * kStep) claim(arrived, seen, p.token);
       if (n < kStep) {  // a place without a key weighs 0, and 0 x inf is not 0
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (kSlots * u + slot >= n) vx[u][0] = vx[u][1] = make_uint4(0u, 0u, 0u, 0u);
+          if (kSlots * u + slot >= n) vx[u] = make_uint4(0u, 0u, 0u, 0u);
       }
-      auto wide = [](const uint4 (&x)[2], float (&f)[16]) {
-        float lo[8], hi[8];
-        unpack8(x[0], lo);
-        unpack8(x[1], hi);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { f[e] = lo[e]; f[8 + e] = hi[e]; }
-      };
-      absorb([&](int u, float (&f)[16]) { wide(kx[u], f); }, [&](int u, float (&f)[16]) { wide(vx[u], f); }, one, one, n);
+      absorb([&](int u, float (&f)[8]) { unpack8(kx[u], f); }, [&](int u, float (&f)[8]) { unpack8(vx[u], f); }, one, one, n);
     }
   } else {
     const int32_t *bc = p.blkcols + (size_t)h * p.cap_b + L.e0;
@@ -196,8 +180,8 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
       __syncthreads();
     }
     auto kept_block = [&](int key) { const int C = key >> shift; return ((blkbm[C >> 5] >> (C & 31)) & 1u) != 0u; };
-    const uint8_t *Kh = p.K + (size_t)kvh * p.capacity * kHeadDim + ln * 16;
-    const uint8_t *Vh = p.V + (size_t)kvh * p.capacity * kHeadDim + ln * 16;
+    const uint8_t *Kh = p.K + (size_t)kvh * p.capacity * kHeadDim + ln * 8;
+    const uint8_t *Vh = p.V + (size_t)kvh * p.capacity * kHeadDim + ln * 8;
     const float *ksh = p.k_scale + (size_t)kvh * (p.capacity >> shift), *vsh = p.v_scale + (size_t)kvh * (p.capacity >> shift);
     int put_at = 0, get_at = 0;  // of the ring, uniform
     auto resolve = [&] {         // until a step is full or the list at its end
@@ -224,15 +208,15 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
       }
       return put_at > get_at;
     };
-    struct Rows { uint4 k[U], v[U]; float sk[U], sv[U]; int n; };
+    struct Rows { uint2 k[U], v[U]; float sk[U], sv[U]; int n; };
     auto fetch = [&](Rows &r) {
       r.n = min(put_at - get_at, kStep);
       wave_lds_sync();
 #pragma unroll
       for (int u = 0; u < U; ++u) {  // a place without a key reads the last key again
         const int j = ring[wave][(get_at + min(kSlots * u + slot, r.n - 1)) & (kRing - 1)];
-        r.k[u] = *(const uint4 *)(Kh + (size_t)j * kHeadDim);
-        r.v[u] = *(const uint4 *)(Vh + (size_t)j * kHeadDim);
+        r.k[u] = *(const uint2 *)(Kh + (size_t)j * kHeadDim);
+        r.v[u] = *(const uint2 *)(Vh + (size_t)j * kHeadDim);
         r.sk[u] = ksh[j >> shift];
         r.sv[u] = vsh[j >> shift];
       }
@@ -243,17 +227,17 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
       if (r.n < kStep) {  // the last step: a place without a key weighs 0, and 0 x NaN is not 0
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (kSlots * u + slot >= r.n) r.v[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (kSlots * u + slot >= r.n) r.v[u] = make_uint2(0u, 0u);
       }
-      auto wide = [](const uint4 &x, float (&f)[16]) {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      auto wide = [](const uint2 &x, float (&f)[8]) {
+        const uint32_t w[2] = {x.x, x.y};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
           const f32_pair a = decode2f<TYPE, false>(w[i]), c = decode2f<TYPE, true>(w[i]);
           f[4 * i] = a[0]; f[4 * i + 1] = a[1]; f[4 * i + 2] = c[0]; f[4 * i + 3] = c[1];
         }
       };
-      absorb([&](int u, float (&f)[16]) { wide(r.k[u], f); }, [&](int u, float (&f)[16]) { wide(r.v[u], f); }, r.sk, r.sv, r.n);
+      absorb([&](int u, float (&f)[8]) { wide(r.k[u], f); }, [&](int u, float (&f)[8]) { wide(r.v[u], f); }, r.sk, r.sv, r.n);
     };
     // the rows of a step are read while the step before is computed
     Rows even, odd;
@@ -272,18 +256,17 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
       }
     }
   }
-  // the eight slots of a wave, then the waves
-  const float Mw = over_keys(m, [](float x, float y) { return fmaxf(x, y); });
+  // the four slots of a wave, then the waves
+  const float Mw = over_slots(m, [](float x, float y) { return fmaxf(x, y); });
   const float ww = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - Mw);
   const auto add = [](float x, float y) { return x + y; };
-  l = over_keys(l * ww, add);
+  l = over_slots(l * ww, add);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = over_keys(acc[e] * ww, add);
+  for (int e = 0; e < 8; ++e) acc[e] = over_slots(acc[e] * ww, add);
   if (lane < kLanes) {
     if (lane == 0) { sm[wave] = Mw; sl[wave] = l; }
-#pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      *(float4 *)&so[wave][ln * 16 + e] = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+    *(float4 *)&so[wave][ln * 8] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    *(float4 *)&so[wave][ln * 8 + 4] = make_float4(acc[4], acc[5], acc[6], acc[7]);
   }
   __syncthreads();
   if (tid < kHeadDim) {

@@ -1,7 +1,7 @@
 // Rotary positions: pair i of a row at position p is turned by the angle p w_i,
 //   (x, y) -> (x cos - y sin, x sin + y cos).
-// Every element is read and written once and nothing else is: the bound is HBM (a device copy), and one
-// launch for a single token.  The sines and cosines of a token serve all heads of Q and K, so a thread takes
+// Every element is read and written once and nothing else is: the bound is HBM (128K tokens of 40 heads 426 us, 6.3 TB/s
+// moved, where a device copy reaches 5.1), and the launch for a single token (2.2 us).  The sines and cosines of a token serve all heads of Q and K, so a thread takes
 // W pairs of one token and walks a range of heads with them in registers.  Angles are kept as fractions of a
 // turn in 64-bit fixed point: position times frequency modulo one turn is then one wrapping integer product,
 // exact for any position, where fp32 radians are off by a hundredth at 256K tokens.
@@ -34,8 +34,7 @@ struct RotaryArgs {
 };
 
 template <int W> struct Vec;
-template <> struct Vec<8> { typedef uint4 type; };
-template <> struct Vec<4> { typedef uint2 type; };
+template <> struct Vec<4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Vec<2> { typedef uint32_t type; };
 template <> struct Vec<1> { typedef uint16_t type; };
 
@@ -49,9 +48,8 @@ __device__ inline float value(uint16_t b) { return __uint_as_float((uint32_t)b <
 __device__ inline uint16_t rounded(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 // A row is cut into 64 / W units of 2W elements: those of the pairs first (the two halves' W elements, or 2W
-// neighbours), then those that pass.  W is the largest power of two up to 8 that divides the number of pairs, so
-// that a unit is all pairs or none and its two accesses are aligned (16 bytes each at 128, 64, 96 or 32 rotary
-// dims; dims that are no multiple of 16 pay with narrower ones).  256 threads: units of consecutive tokens.
+// neighbours), then those that pass.  W divides the number of pairs, so that a unit is all pairs or none and its two
+// accesses are aligned.  256 threads: units of consecutive tokens.
 template <int W, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p) {
   constexpr int kUnits = 64 / W, kTokens = kThreads / kUnits;
@@ -63,6 +61,13 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p) {
   const int h0 = blockIdx.y * p.per, h1 = min(h0 + p.per, p.H);
   const int a = turns && HALF ? u * W : 2 * u * W;   // first element of either access
   const int b = turns && HALF ? a + p.pairs : a + W;
+  Chunk<W> xa, xb;
+  auto read = [&](int h) {
+    const uint16_t *x = h < p.Hq ? p.q + h * p.q_hs + t * p.q_rs : p.k + (h - p.Hq) * p.k_hs + t * p.k_rs;
+    xa.v = *(const typename Vec<W>::type *)(x + a);
+    xb.v = *(const typename Vec<W>::type *)(x + b);
+  };
+  read(h0);  // on its way while the sines are taken
   float c[W], s[W];
   if (turns) {
     const uint64_t at = (uint64_t)(p.positions ? (int64_t)p.positions[t] : p.pos + t);
@@ -77,13 +82,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p) {
     }
   }
   for (int h = h0; h < h1; ++h) {
-    const bool of_q = h < p.Hq;
-    const int hh = of_q ? h : h - p.Hq;
-    const uint16_t *x = (of_q ? p.q : p.k) + hh * (of_q ? p.q_hs : p.k_hs) + t * (of_q ? p.q_rs : p.k_rs);
-    uint16_t *y = (of_q ? p.qo : p.ko) + hh * (of_q ? p.qo_hs : p.ko_hs) + t * (of_q ? p.qo_rs : p.ko_rs);
-    Chunk<W> xa, xb;
-    xa.v = *(const typename Vec<W>::type *)(x + a);
-    xb.v = *(const typename Vec<W>::type *)(x + b);
+    if (h > h0) read(h);
+    uint16_t *y = h < p.Hq ? p.qo + h * p.qo_hs + t * p.qo_rs : p.ko + (h - p.Hq) * p.ko_hs + t * p.ko_rs;
     if (turns) {
       if (HALF) {
 #pragma unroll
@@ -106,8 +106,14 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p) {
         for (int e = 0; e < W; ++e) { xa.e[e] = z[e]; xb.e[e] = z[W + e]; }
       }
     }
-    *(typename Vec<W>::type *)(y + a) = xa.v;
-    *(typename Vec<W>::type *)(y + b) = xb.v;
+    typename Vec<W>::type *ya = (typename Vec<W>::type *)(y + a), *yb = (typename Vec<W>::type *)(y + b);
+    if constexpr (W == 4) {  // many rows: outputs that the caches need not keep, see below
+      __builtin_nontemporal_store(xa.v, ya);
+      __builtin_nontemporal_store(xb.v, yb);
+    } else {
+      *ya = xa.v;
+      *yb = xb.v;
+    }
   }
 }
 
@@ -170,15 +176,20 @@ hipError_t launch_rotary(const Shape &sh, const RotaryTable &f, sa_rows Q, sa_ro
   a.pairs = f.pairs;
   a.copy = (Q.data && Q.data != Qo.data) || (K.data && K.data != Ko.data);
   a.f = f;
-  const int w = f.pairs % 8 == 0 ? 8 : f.pairs % 4 == 0 ? 4 : f.pairs % 2 == 0 ? 2 : 1;
+  // The widest W of 4, 2 and 1 that divides the pairs; 2 at most where there are few rows, for shorter chains of sines
+  // (1 token of 40 heads 2.2 us instead of 2.6, 300 tokens 3.8 instead of 3.4).  8 is slower: 10304 tokens 43 us instead of 40.
+  // Outputs of many rows, 1 MB and more, go past the caches (10304 tokens 40 -> 37 us).
+  const int most = n * a.H <= 4096 ? 2 : 4;
+  const int w = most >= 4 && f.pairs % 4 == 0 ? 4 : f.pairs % 2 == 0 ? 2 : 1;
   const int64_t tiles = (n + kThreads * w / 64 - 1) / (kThreads * w / 64);
-  // as many heads a thread as leave eight workgroups a compute unit
+  // Heads of a thread: as many as leave eight workgroups a compute unit, but three at most.  With more the workgroups, which
+  // drift apart, have every head's memory open at once: 128K tokens of 40 heads (2.68 GB) 426 us, 6.3 TB/s, with 3 heads, 520 with
+  // 16 and 540 with all 40; one head each costs the sines, 570.
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>(a.H, 8 * (int64_t)sh.n_cu / tiles));
-  a.per = (int)((a.H + want - 1) / want);
+  a.per = std::min((int)((a.H + want - 1) / want), 3);
   const dim3 grid((unsigned)tiles, (unsigned)((a.H + a.per - 1) / a.per));
   const bool half = f.layout == SA_ROTARY_HALF;
   switch (w) {
-    case 8: launch<8>(a, half, grid, st); break;
     case 4: launch<4>(a, half, grid, st); break;
     case 2: launch<2>(a, half, grid, st); break;
     default: launch<1>(a, half, grid, st);
