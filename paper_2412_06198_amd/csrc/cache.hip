@@ -6,7 +6,8 @@
 // a key out of the cache is a bf16 value, and a reader may multiply by s wherever it suits it.  The open block
 // stays bf16 until it is full, so that a token is rounded once, by a scale that fits its whole block, however many
 // calls bring the block.
-// Every value is read once and written once: the bound is HBM.  A workgroup holds a block of one head in registers
+// Every value is read once and written once: the bound is HBM (128K tokens of 8 heads, 805 MB, 138 us: 5.8 TB/s; a device copy
+// moves 5.1).  A workgroup holds a block of one head in registers
 // (16 or 32 KB), takes the largest magnitude and writes codes, so nothing is read twice.
 #include "cache_codes.h"
 #include "sa_internal.h"
@@ -29,6 +30,7 @@ struct AppendArgs {
 };
 
 struct Piece { uint4 x[2]; };
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ inline uint32_t max_halves(uint32_t a, uint32_t b) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -120,12 +122,13 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs p) {
   uint8_t *codes = p.codes[side] + ((int64_t)h * p.capacity + (block << p.shift)) * kHeadDim;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    uint4 y;
-    y.x = encode4<TYPE>(x[i].x[0].x, x[i].x[0].y, inverse);
-    y.y = encode4<TYPE>(x[i].x[0].z, x[i].x[0].w, inverse);
-    y.z = encode4<TYPE>(x[i].x[1].x, x[i].x[1].y, inverse);
-    y.w = encode4<TYPE>(x[i].x[1].z, x[i].x[1].w, inverse);
-    *(uint4 *)(codes + (kPieceRows * i + row) * kHeadDim + el) = y;
+    u32x4 y;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      y[2 * k] = encode4<TYPE>(x[i].x[k].x, x[i].x[k].y, inverse);
+      y[2 * k + 1] = encode4<TYPE>(x[i].x[k].z, x[i].x[k].w, inverse);
+    }
+    __builtin_nontemporal_store(y, (u32x4 *)(codes + (kPieceRows * i + row) * kHeadDim + el));  // 144 -> 138 us at 128K tokens
   }
   if (tid == 0) p.scale[side][h * (p.capacity >> p.shift) + block] = __uint_as_float((uint32_t)(127 + e) << 23);
   if (block == first && in_turn) copy(last, last << p.shift, p.end);

@@ -33,7 +33,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
-constexpr int kMaxSplits = 64;
+constexpr int kMaxSplits = 256;
 constexpr int kRowsMany = 128, kRowsFew = 32;  // query rows of a workgroup
 
 struct AttendArgs {
@@ -690,43 +690,56 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
 }
 
 // The splits of a row joined: WAVES waves per row, each every WAVES-th split, two outputs a lane, the reads of eight
-// splits in flight.  One wave and a split after the other took 19 us for 32 rows of 64 splits.
+// splits in flight.  One wave and a split after the other took 19 us for 32 rows of 64 splits.  (The workgroup of a KV head that
+// arrives last could join in the first launch: 0.4 to 5 us slower from 300 to 8000 keys, since it alone reads what this launch
+// spreads.)
 template <int WAVES>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
-  __shared__ float2 part[kThreads / 64][64];
+  constexpr int kPer = WAVES == 1 ? 1 : kMaxSplits / 64;  // splits of a lane
+  __shared__ float2 sums[kThreads / 64][64];
+  __shared__ float weights[kThreads / 64][64 * kPer];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k0 = wave % WAVES;
   const int all = p.Hkv * p.rows, at = min((int)blockIdx.x * (kThreads / 64 / WAVES) + wave / WAVES, all - 1);  // KV head, row
-  const float2 ml = lane < p.S ? p.ml[(size_t)at * p.S + lane] : make_float2(-INFINITY, 0.f);
+  float2 ml[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) ml[i] = lane + 64 * i < p.S ? p.ml[(size_t)at * p.S + lane + 64 * i] : make_float2(-INFINITY, 0.f);
   const float *src = p.part + (size_t)at * p.S * kHeadDim + 2 * lane;
   float2 o = make_float2(0.f, 0.f), x[8];
-  float w = 0.f, L = 0.f;
+  float L = 0.f;
   for (int s0 = k0; s0 < p.S; s0 += 8 * WAVES) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (s0 + i * WAVES < p.S) x[i] = *(const float2 *)(src + (size_t)(s0 + i * WAVES) * kHeadDim);
     if (s0 == k0) {  // once, with the first reads on their way
-      float M = ml.x;
+      float M = ml[0].x;
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) M = fmaxf(M, ml[i].x);
       for (int e = 32; e >= 1; e >>= 1) M = fmaxf(M, __shfl_xor(M, e));
-      w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-      L = ml.y * w;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const float w = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - M);
+        weights[wave][lane + 64 * i] = w;
+        L += ml[i].y * w;
+      }
       for (int e = 32; e >= 1; e >>= 1) L += __shfl_xor(L, e);
+      wave_lds_sync();
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (s0 + i * WAVES < p.S) {
-        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s0 + i * WAVES));
-        o.x = __builtin_fmaf(x[i].x, ws, o.x);
-        o.y = __builtin_fmaf(x[i].y, ws, o.y);
+        const float w = weights[wave][s0 + i * WAVES];
+        o.x = __builtin_fmaf(x[i].x, w, o.x);
+        o.y = __builtin_fmaf(x[i].y, w, o.y);
       }
   }
   if (WAVES > 1) {
-    part[wave][lane] = o;
+    sums[wave][lane] = o;
     __syncthreads();
     if (k0 != 0) return;
 #pragma unroll
     for (int k = 1; k < WAVES; ++k) {
-      o.x += part[wave + k][lane].x;
-      o.y += part[wave + k][lane].y;
+      o.x += sums[wave + k][lane].x;
+      o.y += sums[wave + k][lane].y;
     }
   }
   const int kvh = at / p.rows, row = at - kvh * p.rows, tok = row / p.g;
@@ -756,9 +769,13 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   const bool few = a.rows <= kRowsFew;
   const int per_wg = few ? kRowsFew : kRowsMany;
   a.tiles = (a.rows + per_wg - 1) / per_wg;
-  // Splits of the keys: two workgroups a compute unit in all, 128 (few rows) or 256 keys a workgroup at least.
-  const int64_t wgs = (int64_t)a.tiles * sh.Hkv, least = few ? 128 : 256;
-  int64_t S = 2 * (int64_t)sh.n_cu / wgs;
+  // Splits of the keys.  Many rows: two workgroups a compute unit in all, 256 keys each at least (128: 1 to 2 us faster for 40 rows
+  // or less than 300 keys, up to 4 slower for 64 rows and 4K).  Few rows: one a compute unit, and two where that leaves more
+  // than 2048 keys each (32 heads, one token: 8K keys 9.7 us with one and 11.2 with two, 128K 60 and 54), 128 keys each at least; up to 256
+  // keys in all by one (200 keys 6.9 us, 8.4 in splits).
+  const int64_t wgs = (int64_t)a.tiles * sh.Hkv, least = few ? a.tokens <= 256 ? 256 : 128 : 256;
+  int64_t S = std::max<int64_t>(1, sh.n_cu / wgs);
+  if (!few || a.tokens > 2048 * S) S = 2 * (int64_t)sh.n_cu / wgs;
   S = std::min<int64_t>(S, (a.tokens + least - 1) / least);
   S = std::min<int64_t>(S, (int64_t)(max_slots(sh) / ((size_t)a.rows * sh.Hkv)));
   a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
