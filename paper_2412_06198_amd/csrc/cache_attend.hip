@@ -3,14 +3,13 @@
 //
 // The g query heads of a KV head read the same keys, so its g n query rows (token, head of the group) are taken
 // together, 32 to a wave: a decode step of 8 heads a group fills 8 rows of one wave's products, a chunk of a prompt
-// fills workgroups of 128 rows.  Keys are walked in tiles.  Codes come from memory as they are, half the
-// bytes of bf16, and are turned into bf16 (exactly: code times a power of two) on their way into LDS, once per
-// workgroup; from there on it is the tile step of the sparse prefill: S^T = K Q^T with v_mfma_f32_32x32x16_bf16, so
-// that a lane owns a query row, and O^T += V^T P^T with transposing LDS reads.
-//
-// Two shapes of a workgroup (4 waves):
-//   many rows (WQ = 4)  each wave 32 of 128 rows, tiles of 64 keys shared by the four, two tiles in LDS in turn
-//   few rows (WQ = 1)   one set of up to 32 rows, each wave every fourth tile of 32 keys in LDS of its own, no barriers
+// fills workgroups of 128 rows.  The tile step is that of the sparse prefill: S^T = K Q^T, so that a lane owns a query row,
+// and O^T += V^T P^T in v_mfma_f32_32x32x16_bf16 with transposing LDS reads.  Two shapes of a workgroup (4 waves):
+//   few rows   one set of 32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory;
+//              one token of 32 heads at 128K keys (270 MB) 54 us, 5.0 TB/s
+//   many rows  each wave 32 of 128 rows, tiles of 64 keys shared by the four, K in codes for the 8-bit products.  Bound: matrix
+//              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 ms,
+//              1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
 // and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
 // launch.
 #include <algorithm>
@@ -228,8 +227,8 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
   }
 }
 
-// Few rows: one set of up to 32 query rows, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers on
-// the way.  K and V become bf16 on their way into LDS, from registers that were read a tile ahead.
+// Few rows: one set of 32 query rows a workgroup, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers
+// on the way.  K and V become bf16 on their way into LDS, from registers that were read a tile ahead.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
@@ -241,16 +240,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // KV heads side by side, then splits; a single row tile
-  const int kvh = blockIdx.x % p.Hkv, sp = blockIdx.x / p.Hkv;
-  const int t_masked = (p.pos + 1) / KT;  // first tile that some rows do not see
-  const int n_tiles = (p.tokens - 1) / KT + 1;
+  // KV heads side by side, then splits, then row tiles
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = rest / p.S * kRowsFew;
+  const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
+  const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
+  const int n_tiles = (p.pos + (min(r0 + kRowsFew, p.rows) - 1) / p.g) / KT + 1;
   const int per = (n_tiles + p.S - 1) / p.S;
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
   const int n_closed = p.closed / KT;
 
   // this lane's row, and the last key that it sees
-  const int row = min(q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
+  const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim;
   const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
       if (i + 4 < 8) kf[i & 3] = SA_KFRAG(Kt, 0, i + 4);
       __builtin_amdgcn_sched_barrier(0);
     }
-    absorb_tile(sacc, j0 + KT - 1 > p.pos, see - j0 - 4 * gg, lds[wave][1], vbase, p.c, m_run, lacc, oacc);
+    absorb_tile(sacc, j0 + KT - 1 > seen_all, see - j0 - 4 * gg, lds[wave][1], vbase, p.c, m_run, lacc, oacc);
   };
 
   if (t_begin + wave < t_end) fetch(t_begin + wave);
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
           make_float4(oacc[db][r], oacc[db][r + 1], oacc[db][r + 2], oacc[db][r + 3]);
   __syncthreads();
   const int mr = tid >> 3, d0 = (tid & 7) * 16;  // 16 outputs of a row each
-  const int orow = mr;
+  const int orow = r0 + mr;
   if (orow < p.rows) {
     float M = -INFINITY, L = 0.f, w[4];
 #pragma unroll
@@ -766,18 +766,27 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   a.shift = sh.b == 128 ? 7 : 6;
   a.pos = pos; a.tokens = pos + n; a.closed = a.tokens >> a.shift << a.shift;
   a.c = sh.scale * 1.4426950408889634f;
-  const bool few = a.rows <= kRowsFew;
+  // Which shape: few rows a workgroup read the keys again for every 32 rows, many rows walk their tiles one after the other.  The
+  // former where one set holds all rows, and up to 600 thousand keys read in all (5 tokens of 8 heads at 10K keys 13.7 -> 11.4 us, 800
+  // rows of 200 keys 10.7 -> 7.7, 400 rows of 10K 26.0 -> 21.2; beyond, 96 rows of 8 KV heads at 32K keys, 787 thousand, 31.8 -> 35.8).
+  const bool few = a.rows <= kRowsFew || (int64_t)((a.rows + kRowsFew - 1) / kRowsFew) * sh.Hkv * a.tokens <= 600000;
   const int per_wg = few ? kRowsFew : kRowsMany;
   a.tiles = (a.rows + per_wg - 1) / per_wg;
-  // Splits of the keys.  Many rows: two workgroups a compute unit in all, 256 keys each at least (128: 1 to 2 us faster for 40 rows
-  // or less than 300 keys, up to 4 slower for 64 rows and 4K).  Few rows: one a compute unit, and two where that leaves more
-  // than 2048 keys each (32 heads, one token: 8K keys 9.7 us with one and 11.2 with two, 128K 60 and 54), 128 keys each at least; up to 256
-  // keys in all by one (200 keys 6.9 us, 8.4 in splits).
-  const int64_t wgs = (int64_t)a.tiles * sh.Hkv, least = few ? a.tokens <= 256 ? 256 : 128 : 256;
+  // Splits of the keys.  Many rows: two workgroups a compute unit in all, 256 keys each at least, or 128 and 64 where that leaves
+  // the second launch few partial rows (10240, 4096) to join: a lone workgroup takes 1 us a tile (64 rows at 2K keys 14.2 us with
+  // 256, 9.9 with 64; 512 rows at 4K 15.0 and 19.3).  Few rows: one a compute unit, and two where that leaves more than 2048 keys
+  // each (32 heads, one token: 8K keys 9.7 us with one and 11.2 with two, 128K 60 and 54), 128 keys each at least; up to 256 keys in
+  // all by one (200 keys 6.9 us, 8.4 in splits).
+  const int64_t wgs = (int64_t)a.tiles * sh.Hkv, all = (int64_t)a.rows * sh.Hkv;
+  int64_t least = 256;
+  if (few && a.tokens > 256) least = 128;
+  else if (a.tokens <= 256) least = 256;
+  else if (all * ((a.tokens + 63) / 64) <= 4096) least = 64;
+  else if (all * ((a.tokens + 127) / 128) <= 10240) least = 128;
   int64_t S = std::max<int64_t>(1, sh.n_cu / wgs);
   if (!few || a.tokens > 2048 * S) S = 2 * (int64_t)sh.n_cu / wgs;
   S = std::min<int64_t>(S, (a.tokens + least - 1) / least);
-  S = std::min<int64_t>(S, (int64_t)(max_slots(sh) / ((size_t)a.rows * sh.Hkv)));
+  S = std::min<int64_t>(S, (int64_t)max_slots(sh) / all);
   a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
@@ -791,9 +800,8 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
     else attend_rows_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
   }
   if (a.S > 1) {
-    const int all = sh.Hkv * a.rows;
-    if (a.S > 8) join_kernel<4><<<all, kThreads, 0, st>>>(a);
-    else join_kernel<1><<<(all + kThreads / 64 - 1) / (kThreads / 64), kThreads, 0, st>>>(a);
+    if (a.S > 8) join_kernel<4><<<(unsigned)all, kThreads, 0, st>>>(a);
+    else join_kernel<1><<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
   }
   return hipGetLastError();
 }
