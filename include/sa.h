@@ -246,7 +246,8 @@ sa_status sa_search_patterns(sa_ctx *ctx, const void *Q, const void *K, const vo
  * Calls that take a number of tokens of their own take their tensors as sa_rows: a DEVICE tensor
  * [heads][n][128] of bf16, its 128 elements adjacent, strides in elements, 0 for both =>
  * contiguous.  The address must be 16-byte aligned, strides positive multiples of 8; any order of heads and
- * rows will do.  The rows of an output must not overlap one another.  These calls run on the current
+ * rows will do.  The rows of an output must not overlap one another.  Token numbers (n, pos) are host values: a call
+ * recorded into a graph repeats them.  These calls run on the current
  * device, which must be the one of the stream and of every pointer, and need no workspace unless they say so. */
 typedef struct {
   void *data;
@@ -299,7 +300,7 @@ void sa_rotary_destroy(sa_rotary *rotary);
  *   pair (x, y) -> (x cos - y sin, x sin + y cos) * amplitude at angle position * w_i.
  * Angles are exact to 2^-32 of a turn at any position; the arithmetic is fp32, rounded to bf16 once.
  * Q_out may be Q with the same strides (in place), likewise K_out; other overlaps are not allowed.
- * Q.data or K.data may be NULL: that side is left out.  0 <= pos, pos + n <= 2^31; n = 0 does nothing. */
+ * Q.data or K.data may be NULL: that side is left out.  n <= 2^25, 0 <= pos, pos + n <= 2^31; n = 0 does nothing. */
 sa_status sa_rotary_embed(sa_ctx *ctx, const sa_rotary *rotary, sa_rows Q, sa_rows K, int64_t n, int64_t pos,
                           const int32_t *positions, sa_rows Q_out, sa_rows K_out, void *hip_stream);
 
@@ -328,7 +329,7 @@ sa_status sa_cache_bytes(const sa_ctx *ctx, int64_t capacity, size_t sizes[6]);
  * that becomes full gets the least power of two s >= 2^-100 with (largest finite magnitude) <= s * (largest of
  * the type), 1 if all its values are 0, and the codes nearest to value / s (ties to even): the bytes depend on
  * the block's values alone, not on how many calls brought them.  NaN stays NaN; an infinity becomes NaN in
- * e4m3, which has none.  pos + n <= capacity; n = 0 does nothing.  The earlier rows of the open block are read
+ * e4m3, which has none.  n <= 2^25, pos + n <= capacity; n = 0 does nothing.  The earlier rows of the open block are read
  * from k_open, v_open, so pos can be taken back inside the open block, but not into a full one. */
 sa_status sa_cache_append(sa_ctx *ctx, const sa_cache *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos,
                           void *hip_stream);

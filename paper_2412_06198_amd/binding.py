@@ -453,6 +453,8 @@ class Session:
         if self._get_device() != device:  # the library launches on the current device
             with self.torch.cuda.device(device):
                 return self.rotate(rotary, Q, K, Q_out, K_out, pos, positions)
+        if Q is None and K is None or (Q is None) != (Q_out is None) or (K is None) != (K_out is None):
+            raise SaError(1, "Q and Q_out, K and K_out go together, and one pair is needed")
         n = (K if Q is None else Q).shape[1]
         q = qo = k = ko = _NO_ROWS
         if Q is not None:
@@ -515,7 +517,8 @@ class Session:
         sa_cache_decode(self.ctx, struct, q, self._index(), pos, o, self._raw_stream(device))
 
     def attend_scratch(self):
-        """The session's scratch of attend(), allocated at the first use and kept."""
+        """The session's scratch of attend(), allocated at the first use and kept: attend() calls that may overlap in time,
+        replays of graphs on several streams among them, need sessions of their own."""
         if self._attend_scratch is None:
             size = sa_cache_attend_scratch_bytes(self.ctx)
             raw = self.torch.empty(size + 256, dtype=self.torch.uint8, device=self.device)

@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/sa.h: argument checks, shape
 // resolution, workspace carving, and the three launch sequences.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -30,7 +31,7 @@ void carve(sa_ctx *c) {
   c->off[6] = o; o += 256;
   c->off[7] = o; o += align256(sa::index_scratch_bytes(s));
   c->off[8] = o; o += align256((size_t)s.Hq * (s.N / 32) * 4);
-  c->off[9] = o; o += align256(sa::decode_partial_bytes(s));
+  c->off[9] = o; o += align256(std::max(sa::decode_partial_bytes(s), sa::cache_decode_partial_bytes(s)));
   c->off[10] = o; o += align256(sa::attn_item_bytes(s));
   c->off[11] = o; o += align256(sa::attn_tile_bytes(s));
   c->ws_bytes = o;
@@ -354,6 +355,8 @@ sa_status sa_sparse_decode_static(sa_ctx *c, const void *q, const void *K, const
                                                 (hipStream_t)stream));
 }
 
+constexpr int64_t kMaxTokens = (int64_t)1 << 25;  // of a call: grids of 2^32 threads are refused by the runtime
+
 // A strided tensor of n rows a head: contiguous strides filled in, or why it cannot be taken.
 static const char *resolve_rows(sa_rows *r, int heads, int64_t n, bool output) {
   if (!r->data) return "null pointer";
@@ -365,7 +368,7 @@ static const char *resolve_rows(sa_rows *r, int heads, int64_t n, bool output) {
   const int64_t most = (int64_t)1 << 55;  // 128 heads and 2^31 rows of it stay addresses
   // the stride of a single row or head is never used
   if (heads == 1) r->head_stride = n * sa::kHeadDim;
-  if (n == 1 && r->row_stride <= 0) r->row_stride = sa::kHeadDim;
+  if (n == 1) r->row_stride = sa::kHeadDim;
   if (r->head_stride < sa::kHeadDim || r->row_stride < sa::kHeadDim || r->head_stride % 8 || r->row_stride % 8 ||
       r->head_stride > most || r->row_stride > most >> 24)
     return "strides must be multiples of 8, at least head_dim";
@@ -382,8 +385,8 @@ sa_status sa_rotary_embed(sa_ctx *c, const sa_rotary *rotary, sa_rows Q, sa_rows
   if (!c) return SA_ERR_INVALID_ARG;
   if (!rotary) return fail(c, SA_ERR_INVALID_ARG, "null pointer");
   const int64_t top = (int64_t)1 << 31;
-  if (n < 0 || n > top || (!positions && (pos < 0 || pos > top - n)))
-    return fail(c, SA_ERR_INVALID_ARG, "0 <= pos and pos + n <= 2^31 are needed");
+  if (n < 0 || n > kMaxTokens || (!positions && (pos < 0 || pos > top - n)))
+    return fail(c, SA_ERR_INVALID_ARG, "0 <= n <= 2^25, 0 <= pos and pos + n <= 2^31 are needed");
   if ((uintptr_t)positions & 3) return fail(c, SA_ERR_INVALID_ARG, "positions must be 4-byte aligned");
   if (n == 0) return SA_OK;  // an empty tensor may have no address
   if (!Q.data && !K.data) return fail(c, SA_ERR_INVALID_ARG, "null pointer");
@@ -425,8 +428,8 @@ static sa_status check_cache(sa_ctx *c, const sa_cache *h, int64_t tokens) {
 
 sa_status sa_cache_append(sa_ctx *c, const sa_cache *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *stream) {
   if (!c) return SA_ERR_INVALID_ARG;
-  if (n < 0 || pos < 0 || n > (int64_t)1 << 30 || pos > (int64_t)1 << 30)
-    return fail(c, SA_ERR_INVALID_ARG, "n and pos must lie in [0, 2^30]");
+  if (n < 0 || pos < 0 || n > kMaxTokens || pos > (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "n must lie in [0, 2^25], pos in [0, 2^30]");
   const sa_status s = check_cache(c, cache, pos + n);
   if (s != SA_OK) return s;
   if (n == 0) return SA_OK;

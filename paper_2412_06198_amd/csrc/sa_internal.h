@@ -71,7 +71,7 @@ struct Workspace {
   float2 *stats;                  // [Hq][64] row constants, where a launch of their own forms them
   uint32_t *colbits;              // [Hq][N/32] membership bitmap of the selected columns
   int32_t *colprefix;             // [Hq][N/32] number of selected columns before each word of colbits
-  float *dec_part;                // [Hq][splits][132] partial (max, sum, output) of the decode step
+  float *dec_part;                // [Hq][splits][132] partial (max, sum, output) of either decode step
   unsigned int *queue;            // [8] work-queue heads of the attention kernel
   void *idx;                      // per-head scratch of the index builder
   uint16_t *kg, *vg;              // [Hq][roundup64(k_v)][kv_rs] gathered K / V rows of the selected columns
@@ -126,7 +126,6 @@ size_t attn_tile_bytes(const Shape &sh);
 // partials: decode_partial_bytes(sh) bytes of device memory (the context's workspace, or the static array)
 hipError_t launch_sparse_decode(const Shape &sh, float *partials, const uint16_t *q, const uint16_t *K,
                                 const uint16_t *V, sa_index idx, int pos, uint16_t *o, hipStream_t st);
-int decode_splits(const Shape &sh);                 // partials of a head that decode_partial_bytes has room for
 uint64_t next_decode_token();                       // of one launch, see decode_common.h
 bool decode_recorded(hipStream_t st);               // whether the stream is being captured
 size_t decode_static_bytes();                       // size of the library's static decode scratch
@@ -138,6 +137,7 @@ hipError_t launch_rotary(const Shape &sh, const RotaryTable &f, sa_rows Q, sa_ro
                          const int32_t *positions, sa_rows Qo, sa_rows Ko, hipStream_t st);
 hipError_t launch_cache_append(const Shape &sh, const sa_cache &c, sa_rows K, sa_rows V, int64_t n, int64_t pos,
                                hipStream_t st);
+size_t cache_decode_partial_bytes(const Shape &sh);
 hipError_t launch_cache_decode(const Shape &sh, float *partials, const sa_cache &c, const uint16_t *q, sa_index idx,
                                int pos, uint16_t *o, hipStream_t st);
 size_t attend_scratch_bytes(const Shape &sh);

@@ -68,7 +68,7 @@ def test_rotary_calls(ctx):
     _refused(1, "pos", call, ctx, rot, ok, ok, -1, 0, None, ok, ok)
     _refused(1, "pos", call, ctx, rot, ok, ok, 4, -1, None, ok, ok)
     _refused(1, "pos", call, ctx, rot, ok, ok, 4, 2 ** 31 - 3, None, ok, ok)
-    _refused(1, "pos", call, ctx, rot, ok, ok, 2 ** 31 + 1, 0, A, ok, ok)
+    _refused(1, "pos", call, ctx, rot, ok, ok, 2 ** 25 + 1, 0, A, ok, ok)
     _refused(1, "positions", call, ctx, rot, ok, ok, 4, 0, A + 2, ok, ok)
     _refused(1, "aligned", call, ctx, rot, _rows(A + 8), ok, 4, 0, None, ok, ok)
     _refused(1, "strides", call, ctx, rot, ok, _rows(A, 1024, 100), 4, 0, None, ok, ok)
@@ -109,7 +109,7 @@ def test_cache_calls(ctx):
     sa.sa_cache_append(ctx, c, _rows(0), _rows(0), 0, 5)
     _refused(3, "room", sa.sa_cache_append, ctx, c, ok, ok, 1, 8192)
     _refused(3, "room", sa.sa_cache_append, ctx, c, ok, ok, 8193, 0)
-    for n, pos in ((-1, 0), (1, -1), (2 ** 62, 2 ** 62), (2 ** 63 - 1, 1)):
+    for n, pos in ((-1, 0), (1, -1), (2 ** 25 + 1, 0), (2 ** 62, 2 ** 62), (2 ** 63 - 1, 1)):
         _refused(1, "pos", sa.sa_cache_append, ctx, c, ok, ok, n, pos)
     _refused(1, "null", sa.sa_cache_append, ctx, None or c, _rows(0), ok, 1, 0)
     _refused(1, "aligned", sa.sa_cache_append, ctx, c, ok, _rows(A + 2), 1, 0)

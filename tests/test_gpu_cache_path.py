@@ -163,7 +163,8 @@ def test_refusals_of_the_session():
     q, k = torch.zeros(4, 3, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 3, 128, dtype=torch.bfloat16, device="cuda")
     other = sa.Session(4, 4, 512, 64, 64, keep=0.3)
     wide = sa.Session(4, 2, 512, 128, 64, keep=0.3)
-    for call in (lambda: ses.rotate(rot, q, k, q, k[:, :2]), lambda: ses.rotate(rot, q, q, q, q), lambda: ses.rotate(rot, q.float(), k, q, k),
+    for call in (lambda: ses.rotate(rot, None, None, None, None), lambda: ses.rotate(rot, q, None, None, None),
+                 lambda: ses.rotate(rot, q, None, q, k), lambda: ses.rotate(rot, q, k, q, k[:, :2]), lambda: ses.rotate(rot, q, q, q, q), lambda: ses.rotate(rot, q.float(), k, q, k),
                  lambda: ses.rotate(rot, q.cpu(), k, q, k), lambda: ses.rotate(rot, q.transpose(1, 2), k, q, k),
                  lambda: ses.rotate(rot, q, k, q, k, positions=torch.zeros(3, dtype=torch.int64, device="cuda")),
                  lambda: ses.rotate(rot, q, k, q, k, positions=torch.zeros(2, dtype=torch.int32, device="cuda")),
