@@ -43,6 +43,7 @@ struct AttendArgs {
   const uint16_t *k_open, *v_open;
   int64_t q_hs, q_rs, o_hs, o_rs, capacity;
   int g, Hkv, rows, tiles, S;  // query heads and query rows of a KV head, row tiles, splits of the keys
+  int turn;                    // row tiles from the last one down, this many, then from the first one up
   int shift;                   // log2 of the block
   int pos, tokens, closed;     // of the first query; in the cache; in its full blocks
   float c;                     // softmax scale * log2(e)
@@ -439,9 +440,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then
-  // row tiles from the last one (the most keys) down.
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, rt = p.tiles - 1 - rest / p.S;
+  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then row tiles
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, down = rest / p.S;
+  const int rt = down < p.turn ? p.tiles - 1 - down : down - p.turn;
   const int r0 = rt * kRowsMany, r_last = min(r0 + kRowsMany, p.rows) - 1;
   const int seen_all = p.pos + r0 / p.g;                 // last key that every row of the workgroup sees
   const int t_masked = (seen_all + 1) / KT;              // first tile that some do not
@@ -788,6 +789,9 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   S = std::min<int64_t>(S, (a.tokens + least - 1) / least);
   S = std::min<int64_t>(S, (int64_t)max_slots(sh) / all);
   a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
+  // Many rows: long row tiles first; where every compute unit gets one workgroup and some a second, the second ones in the
+  // opposite order, so that the longest share theirs with the shortest (2048 tokens of 32 heads at 0: 49.2 -> 46.1 us, at 5K 178 -> 175).
+  a.turn = wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu ? std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S))) : a.tiles;
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
