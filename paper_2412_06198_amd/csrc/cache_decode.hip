@@ -274,16 +274,14 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) M = fmaxf(M, sm[k]);
     float lsum = 0.f, O = 0.f;
-    if (M > -INFINITY) {
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float w = __builtin_amdgcn_exp2f(sm[k] - M);  // 0 for an empty one
-        lsum += sl[k] * w;
-        O += so[k][tid] * w;
-      }
+    for (int k = 0; k < kWaves; ++k) {
+      const float w = sm[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[k] - M);  // no key, or none but NaN: sums of 0 or NaN
+      lsum += sl[k] * w;
+      O += so[k][tid] * w;
     }
     if (L.n == 1) {  // the only workgroup of the head
-      const __bf16 r = (__bf16)(lsum > 0.f ? O / lsum : 0.f);
+      const __bf16 r = (__bf16)(O / lsum);
       p.o[(size_t)h * kHeadDim + tid] = __builtin_bit_cast(uint16_t, r);
     } else {
       float *dst = part + (size_t)sp * kPartStride;
@@ -300,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(CacheDecArgs p) 
   if (counts) s_last = arrive(arrived, p.token, L.n);
   __syncthreads();
   asm volatile("" ::: "memory");
-  if (s_last) merge(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
+  if (s_last) merge<true>(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
 }
 
 // Partials of a head: three workgroups of four waves a compute unit in all.  Two, as in the step on bf16 tensors, are 5 %

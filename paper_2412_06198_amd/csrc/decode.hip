@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void decode_kernel(DecArgs p) {
   }
   __syncthreads();
   asm volatile("" ::: "memory");
-  if (s_last) merge(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
+  if (s_last) merge<false>(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
 }
 
 }  // namespace

@@ -53,7 +53,9 @@ __device__ inline void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMI
 __device__ inline float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // Merge n <= 64 partials of a head, normalise, round to bf16: 256 threads, thread (k0, d) takes the outputs d
-// of partials k0, k0 + 2, ...  All reads are on their way before the first is needed.
+// of partials k0, k0 + 2, ...  All reads are on their way before the first is needed.  A sum that is not positive (NaN
+// among the scores) gives 0, or with KEEP_NAN what the division does.
+template <bool KEEP_NAN>
 __device__ inline void merge(const float *src, int n, float *wgt, float *s_L, float *half, uint16_t *o) {
   const int tid = threadIdx.x, d = tid & 127, k0 = tid >> 7;
   float mk = -INFINITY, lk = 0.f;
@@ -89,7 +91,7 @@ __device__ inline void merge(const float *src, int n, float *wgt, float *s_L, fl
   if (k0) return;
   O += half[d];
   const float L = *s_L;
-  const __bf16 r = (__bf16)(L > 0.f ? O / L : 0.f);
+  const __bf16 r = (__bf16)(KEEP_NAN || L > 0.f ? O / L : 0.f);
   o[d] = __builtin_bit_cast(uint16_t, r);
 }
 

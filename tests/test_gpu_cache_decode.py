@@ -158,3 +158,27 @@ def test_nan_of_kept_and_other_keys():
     bad = np.zeros((2, 128), bool)
     bad[0, 5] = True
     assert (np.isnan(host_f64(o)) == bad).all()
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_nan_scores_of_whole_heads(many):
+    # NaN in every score of a head, of a workgroup or of a wave: the head's output is NaN, the others' are not
+    print(f"case cached decode NaN scores {many}", flush=True)
+    N, b = (8192, 64) if many else (64, 64)
+    pos = N + 40
+    Q, K, V = gen.random_qkv(4, 2, pos + 1, 128, seed=332)
+    ses = sa.Session(4, 2, N, b, 64, keep=0.9)
+    ses.estimate(dev_bf16(Q)[:, :N].contiguous(), dev_bf16(K)[:, :N].contiguous())
+    ses.build_index([1, 1, 1, 1])
+    K[1, :512 if many else 64, 7] = 0x7FC0
+    c = ses.cache(N + 64)
+    ses.append(c, dev_bf16(K), dev_bf16(V), 0)
+    q = dev_bf16(Q)[:, pos].contiguous()
+    q[1, 9] = float("nan")
+    o = torch.empty_like(q)
+    ses.decode_cached(c, q, pos, o)
+    torch.cuda.synchronize()
+    index = download_index(ses)
+    bad = [False, True] + [bool((np.asarray(dec.kept_keys(index, h, N, b, pos)) < (512 if many else 64)).any()) for h in (2, 3)]
+    assert bad[2] and bad[3]
+    assert (np.isnan(host_f64(o)) == np.array(bad)[:, None]).all()
