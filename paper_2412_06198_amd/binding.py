@@ -315,6 +315,8 @@ class Cache:
     k_scale, v_scale fp32 [n_kv_heads, capacity / block], k_open, v_open bf16 [n_kv_heads, block, 128], contiguous."""
 
     def __init__(self, k, v, k_scale, v_scale, k_open, v_open, cache_type=SA_CACHE_E4M3):
+        if k.ndim != 3 or k_open.ndim != 3 or k_open.shape[1] == 0:
+            raise SaError(1, "k and k_open of a cache are [n_kv_heads, capacity, 128] and [n_kv_heads, block, 128]")
         heads, capacity, d = k.shape
         block = k_open.shape[1]
         want = [(heads, capacity, d)] * 2 + [(heads, capacity // block)] * 2 + [(heads, block, d)] * 2

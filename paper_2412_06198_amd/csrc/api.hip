@@ -474,6 +474,8 @@ sa_status sa_cache_attend(sa_ctx *c, const sa_cache *cache, sa_rows Q, int64_t n
   const char *why = resolve_rows(&Q, c->sh.Hq, n, false);
   if (!why) why = resolve_rows(&O, c->sh.Hq, n, true);
   if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  if (Q.data == O.data && (Q.head_stride != O.head_stride || Q.row_stride != O.row_stride))
+    return fail(c, SA_ERR_INVALID_ARG, "in place, the strides must be the same");
   return hip_result(c, sa::launch_cache_attend(c->sh, *cache, Q, (int)n, (int)pos, O, scratch, (hipStream_t)stream));
 }
 

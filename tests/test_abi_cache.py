@@ -137,6 +137,18 @@ def test_attend_calls(ctx):
     _refused(3, "room", call, ctx, c, ok, 2, 8191, ok, A, size)
     _refused(1, "null", call, ctx, c, _rows(0), 1, 0, ok, A, size)
     _refused(1, "overlap", call, ctx, c, ok, 4, 0, _rows(2 * A, 384, 128), A, size)
+    _refused(1, "in place", call, ctx, c, ok, 4, 0, _rows(A, 1024, 128), A, size)
+
+
+@pytest.mark.parametrize("bad", [dict(k=(8192, 128)), dict(k_open=(256,)), dict(k_open=(2, 0, 128)), dict(v=(2, 8192, 64)), dict(k_scale=(2, 127))])
+def test_buffers_of_a_cache(bad):
+    torch = pytest.importorskip("torch")
+    shapes = dict(k=(2, 8192, 128), v=(2, 8192, 128), k_scale=(2, 128), v_scale=(2, 128), k_open=(2, 64, 128), v_open=(2, 64, 128))
+    kinds = dict(k=torch.uint8, v=torch.uint8, k_scale=torch.float32, v_scale=torch.float32, k_open=torch.bfloat16, v_open=torch.bfloat16)
+    sa.Cache(**{name: torch.empty(shapes[name], dtype=kinds[name]) for name in shapes})
+    shapes.update(bad)
+    with pytest.raises(sa.SaError):
+        sa.Cache(**{name: torch.empty(shapes[name], dtype=kinds[name]) for name in shapes})
 
 
 def test_null_context_and_handles():
