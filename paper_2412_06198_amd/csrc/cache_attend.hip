@@ -690,28 +690,38 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
   if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, row, head, tok, sp, gg, m_run, l_run, oacc);
 }
 
-// The splits of a row joined: WAVES waves per row, each every WAVES-th split, two outputs a lane, the reads of eight
-// splits in flight.  One wave and a split after the other took 19 us for 32 rows of 64 splits.  (The workgroup of a KV head that
-// arrives last could join in the first launch: 0.4 to 5 us slower from 300 to 8000 keys, since it alone reads what this launch
-// spreads.)
-template <int WAVES>
+// The splits of a row joined: WAVES waves per row, the reads of IN splits of a lane in flight at once.  1 wave: two outputs a lane;
+// 4: half a wave a split, four outputs a lane.  The bound is the launch and one round trip to memory, since the partial rows come
+// from other XCDs.  Hence (4, 16) beyond 32 splits, 128 of them in flight (against 32: 5 tokens of 8 heads at 10K keys, 81 splits,
+// 11.3 -> 10.2 us, one token at 30K, 235 splits, 14.6 -> 11.6), and (4, 4) up to 32, where there may be thousands of rows and
+// its registers would keep waves away (100 tokens of 32 heads at 10K keys, 16 splits, 33.8 us instead of 36.0).
+// (The workgroup of a KV head that arrives last could join in the first launch: 0.4 to 5 us slower from 300 to 8000 keys,
+// since it alone reads what this launch spreads.)
+template <int WAVES, int IN>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
-  constexpr int kPer = WAVES == 1 ? 1 : kMaxSplits / 64;  // splits of a lane
-  __shared__ float2 sums[kThreads / 64][64];
+  constexpr int kSide = WAVES == 1 ? 1 : 2;               // splits that a wave reads side by side
+  constexpr int kPer = WAVES == 1 ? 1 : kMaxSplits / 64;  // splits whose weight a lane takes
+  constexpr int W = 2 * kSide, kLanes = kHeadDim / W;
+  typedef float vec __attribute__((ext_vector_type(W)));
+  typedef __bf16 bvec __attribute__((ext_vector_type(W)));
+  __shared__ vec sums[kThreads / 64][kLanes];
   __shared__ float weights[kThreads / 64][64 * kPer];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k0 = wave % WAVES;
+  const int lane = threadIdx.x & 63, side = lane / kLanes, ln = lane % kLanes;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k0 = wave % WAVES;
   const int all = p.Hkv * p.rows, at = min((int)blockIdx.x * (kThreads / 64 / WAVES) + wave / WAVES, all - 1);  // KV head, row
   float2 ml[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) ml[i] = lane + 64 * i < p.S ? p.ml[(size_t)at * p.S + lane + 64 * i] : make_float2(-INFINITY, 0.f);
-  const float *src = p.part + (size_t)at * p.S * kHeadDim + 2 * lane;
-  float2 o = make_float2(0.f, 0.f), x[8];
+  const float *src = p.part + (size_t)at * p.S * kHeadDim + W * ln;
+  vec o = {}, x[IN];
   float L = 0.f;
-  for (int s0 = k0; s0 < p.S; s0 += 8 * WAVES) {
+  for (int s0 = kSide * k0; s0 < p.S; s0 += kSide * WAVES * IN) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (s0 + i * WAVES < p.S) x[i] = *(const float2 *)(src + (size_t)(s0 + i * WAVES) * kHeadDim);
-    if (s0 == k0) {  // once, with the first reads on their way
+    for (int i = 0; i < IN; ++i) {
+      const int s = s0 + kSide * WAVES * i;
+      if (s < p.S) x[i] = *(const vec *)(src + (size_t)min(s + side, p.S - 1) * kHeadDim);
+    }
+    if (s0 == kSide * k0) {  // once, with the first reads on their way
       float M = ml[0].x;
 #pragma unroll
       for (int i = 1; i < kPer; ++i) M = fmaxf(M, ml[i].x);
@@ -726,26 +736,33 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
       wave_lds_sync();
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (s0 + i * WAVES < p.S) {
-        const float w = weights[wave][s0 + i * WAVES];
-        o.x = __builtin_fmaf(x[i].x, w, o.x);
-        o.y = __builtin_fmaf(x[i].y, w, o.y);
+    for (int i = 0; i < IN; ++i) {
+      const int s = s0 + kSide * WAVES * i;
+      if (s < p.S) {
+        if (s + side >= p.S) x[i] = vec{};  // no split: 0 x inf is not 0
+        const float w = weights[wave][min(s + side, p.S - 1)];
+#pragma unroll
+        for (int e = 0; e < W; ++e) o[e] = __builtin_fmaf(x[i][e], w, o[e]);
       }
+    }
+  }
+  if (kSide == 2) {
+#pragma unroll
+    for (int e = 0; e < W; ++e) o[e] = sum_pair(o[e]);
   }
   if (WAVES > 1) {
-    sums[wave][lane] = o;
+    if (side == 0) sums[wave][ln] = o;
     __syncthreads();
     if (k0 != 0) return;
 #pragma unroll
-    for (int k = 1; k < WAVES; ++k) {
-      o.x += sums[wave + k][lane].x;
-      o.y += sums[wave + k][lane].y;
-    }
+    for (int k = 1; k < WAVES; ++k) o += sums[wave + k][ln];
   }
+  if (side != 0) return;
   const int kvh = at / p.rows, row = at - kvh * p.rows, tok = row / p.g;
-  const bf16x2 r = {(__bf16)(o.x / L), (__bf16)(o.y / L)};
-  *(uint32_t *)(p.O + (size_t)(kvh * p.g + row - tok * p.g) * p.o_hs + (size_t)tok * p.o_rs + 2 * lane) = __builtin_bit_cast(uint32_t, r);
+  bvec r;
+#pragma unroll
+  for (int e = 0; e < W; ++e) r[e] = (__bf16)(o[e] / L);
+  *(bvec *)(p.O + (size_t)(kvh * p.g + row - tok * p.g) * p.o_hs + (size_t)tok * p.o_rs + W * ln) = r;
 }
 
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit.
@@ -804,8 +821,9 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
     else attend_rows_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
   }
   if (a.S > 1) {
-    if (a.S > 8) join_kernel<4><<<(unsigned)all, kThreads, 0, st>>>(a);
-    else join_kernel<1><<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+    if (a.S > 32) join_kernel<4, 16><<<(unsigned)all, kThreads, 0, st>>>(a);
+    else if (a.S > 8) join_kernel<4, 4><<<(unsigned)all, kThreads, 0, st>>>(a);
+    else join_kernel<1, 8><<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
   }
   return hipGetLastError();
 }

@@ -222,3 +222,30 @@ def test_replays(n):
         ses.attend(c, Qd, 1000, want)
         torch.cuda.synchronize()
         assert torch.equal(O, want), rep
+
+
+@pytest.mark.parametrize("parts", [2, 3, 8, 9, 31, 32, 33, 64, 65, 127, 128, 129, 200, 235, 256, 300])
+@pytest.mark.parametrize("heads,n", [((1, 1), 1), ((8, 1), 3), ((5, 5), 2)])
+def test_joins(parts, heads, n):
+    # up to as many splits as there are 128 keys; an infinite value in the first or last of them
+    print(f"case attend join heads={heads} n={n} parts={parts}", flush=True)
+    tokens = 128 * parts - 3
+    if parts % 2 == 0:
+        _check(*_setup(*heads, 64, tokens, seed=parts), n)
+        return
+    at = 5 if parts % 4 == 1 else tokens - 40
+
+    def change(Q, K, V):
+        V[:, at, 9] = 0x7F80
+        V[:, at, 64] = 0xFF80
+
+    ses, c, Q, keys, vals = _setup(*heads, 64, tokens, sa.SA_CACHE_E5M2, parts, change)
+    Qd = dev_bf16(Q[:, tokens - n:])
+    O = torch.full_like(Qd, 7.0)
+    ses.attend(c, Qd, tokens - n, O)
+    got = host_f64(O)
+    assert (got[..., 9] == np.inf).all() and (got[..., 64] == -np.inf).all()
+    vals[:, at, 9] = vals[:, at, 64] = 0
+    want, tol = _reference(_f64(Q[:, tokens - n:]), keys, vals, tokens - n)
+    finite = np.delete(np.arange(128), [9, 64])
+    assert (np.abs(got - want) <= tol)[..., finite].all()
