@@ -13,6 +13,7 @@
 // and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
 // launch.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "cache_codes.h"
@@ -246,7 +247,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
   const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
   const int n_tiles = (p.pos + (min(r0 + kRowsFew, p.rows) - 1) / p.g) / KT + 1;
-  const int per = (n_tiles + p.S - 1) / p.S;
+  int per = (n_tiles + p.S - 1) / p.S;
+  if (per >= 64) per |= 1;  // 256 KB from workgroup to workgroup fall on few memory channels (130000 keys 60.3 us, odd 54.3)
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
   const int n_closed = p.closed / KT;
 
@@ -768,6 +770,50 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit.
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 
+// Which kernel, and into how many splits the keys go.  Both are estimates of the same time, of terms that were each measured with
+// 32 heads over 300 to 130 thousand keys and 1 to 2000 tokens (us):
+//                                            few rows      many rows
+//   start and end                            5             7.3
+//   keys of a tile (few: of all four waves)  128           64
+//   a tile, up to a workgroup a compute unit 1.1           1.1
+//   a tile, two, which share it              1.95          1.3
+//   start of the second one                  1             1
+//   a join: its launch 2.8, and 1 KB written and read for each row and split at 5 TB/s
+// The least of them over no splits, as many as give one or two workgroups a compute unit, and in either range where the
+// join weighs as much as the tiles that it saves.  Over 384 shapes of 8 to 64 heads the choice is 1 % slower than the best of all
+// splits and kernels; fixed limits (600 thousand keys of all sets of 32 rows, 128 or 256 keys a split) were 3 %, and
+// at worst 11.7 us instead of 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6 (500 tokens of 64 heads at 1000).
+struct Plan { bool few; int S; };
+Plan plan_of(const Shape &sh, int rows, int tokens) {
+  Plan best = {true, 1};
+  float least = INFINITY;
+  const int64_t all = (int64_t)rows * sh.Hkv;
+  for (int few = 1; few >= (rows <= kRowsFew ? 1 : 0); --few) {
+    const int per_wg = few ? kRowsFew : kRowsMany, keys = few ? 32 : 64, waves = few ? 4 : 1;  // of a tile; that share out the tiles
+    const int64_t wgs = (rows + per_wg - 1) / per_wg * (int64_t)sh.Hkv;
+    const int tiles = (tokens + keys - 1) / keys;
+    const int top = (int)std::min<int64_t>(std::min(tiles / waves + 1, kMaxSplits), (int64_t)max_slots(sh) / all);
+    auto consider = [&](int64_t splits) {
+      const int S0 = (int)std::max<int64_t>(1, std::min<int64_t>(splits, top));
+      const int share = (tiles + S0 - 1) / S0, S = (tiles + share - 1) / share, per = (share + waves - 1) / waves;
+      const float load = (float)wgs * S / sh.n_cu;
+      float t = few ? 5.f : 7.3f;
+      if (load <= 1.f) t += per * 1.1f;
+      else t += 1.f + per * (few ? 1.95f : 1.3f) * std::max(1.f, load / 2);
+      if (S > 1) t += 2.8f + all * S * 0.0002f;
+      if (t < least) { least = t; best = {few != 0, S}; }
+    };
+    consider(1);
+    for (int two = 0; two < 2; ++two) {
+      const int64_t fill = (two + 1) * (int64_t)sh.n_cu / wgs;
+      const float even = std::sqrt((float)tiles / waves * (!two ? 1.1f : few ? 1.95f : 1.3f) / (all * 0.0002f));
+      consider(fill);
+      consider(std::min<int64_t>(fill, (int64_t)even));
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 size_t attend_scratch_bytes(const Shape &sh) { return max_slots(sh) * (kHeadDim * 4 + 8); }
@@ -784,28 +830,10 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   a.shift = sh.b == 128 ? 7 : 6;
   a.pos = pos; a.tokens = pos + n; a.closed = a.tokens >> a.shift << a.shift;
   a.c = sh.scale * 1.4426950408889634f;
-  // Which shape: few rows a workgroup read the keys again for every 32 rows, many rows walk their tiles one after the other.  The
-  // former where one set holds all rows, and up to 600 thousand keys read in all (5 tokens of 8 heads at 10K keys 13.7 -> 11.4 us, 800
-  // rows of 200 keys 10.7 -> 7.7, 400 rows of 10K 26.0 -> 21.2; beyond, 96 rows of 8 KV heads at 32K keys, 787 thousand, 31.8 -> 35.8).
-  const bool few = a.rows <= kRowsFew || (int64_t)((a.rows + kRowsFew - 1) / kRowsFew) * sh.Hkv * a.tokens <= 600000;
-  const int per_wg = few ? kRowsFew : kRowsMany;
-  a.tiles = (a.rows + per_wg - 1) / per_wg;
-  // Splits of the keys.  Many rows: two workgroups a compute unit in all, 256 keys each at least, or 128 and 64 where that leaves
-  // the second launch few partial rows (10240, 4096) to join: a lone workgroup takes 1 us a tile (64 rows at 2K keys 14.2 us with
-  // 256, 9.9 with 64; 512 rows at 4K 15.0 and 19.3).  Few rows: one a compute unit, and two where that leaves more than 2048 keys
-  // each (32 heads, one token: 8K keys 9.7 us with one and 11.2 with two, 128K 60 and 54), 128 keys each at least; up to 256 keys in
-  // all by one (200 keys 6.9 us, 8.4 in splits).
+  const Plan plan = plan_of(sh, a.rows, a.tokens);
+  a.tiles = (a.rows + (plan.few ? kRowsFew : kRowsMany) - 1) / (plan.few ? kRowsFew : kRowsMany);
+  a.S = plan.S;
   const int64_t wgs = (int64_t)a.tiles * sh.Hkv, all = (int64_t)a.rows * sh.Hkv;
-  int64_t least = 256;
-  if (few && a.tokens > 256) least = 128;
-  else if (a.tokens <= 256) least = 256;
-  else if (all * ((a.tokens + 63) / 64) <= 4096) least = 64;
-  else if (all * ((a.tokens + 127) / 128) <= 10240) least = 128;
-  int64_t S = std::max<int64_t>(1, sh.n_cu / wgs);
-  if (!few || a.tokens > 2048 * S) S = 2 * (int64_t)sh.n_cu / wgs;
-  S = std::min<int64_t>(S, (a.tokens + least - 1) / least);
-  S = std::min<int64_t>(S, (int64_t)max_slots(sh) / all);
-  a.S = (int)std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
   // Many rows: long row tiles first; where every compute unit gets one workgroup and some a second, the second ones in the
   // opposite order, so that the longest share theirs with the shortest (2048 tokens of 32 heads at 0: 49.2 -> 46.1 us, at 5K 178 -> 175).
   a.turn = wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu ? std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S))) : a.tiles;
@@ -813,7 +841,7 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
   const bool e4m3 = c.type == SA_CACHE_E4M3;
-  if (few) {
+  if (plan.few) {
     if (e4m3) attend_few_kernel<SA_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
     else attend_few_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
   } else {

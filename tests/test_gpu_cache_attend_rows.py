@@ -1,5 +1,5 @@
-"""Causal attention over the 8-bit cache where many keys are read (more than 600 thousand over all sets of 32 rows): workgroups
-of 128 rows, K multiplied as codes, Q cut into two.  Against fp64 on the values that the cache stands for; the reference runs
+"""Causal attention over the 8-bit cache where many rows read many keys (600 thousand and more over all sets of 32 rows), which
+workgroups of 128 rows take, but at the edge: K multiplied as codes, Q cut into two.  Against fp64 on the values that the cache stands for; the reference runs
 on the GPU, one plain product per head.
 
 Tolerance: as in test_gpu_cache_attend.py.  Q = hi + lo is exact, but for elements below 2^-14 of their row's largest, which are
