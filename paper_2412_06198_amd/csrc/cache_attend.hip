@@ -5,13 +5,13 @@
 // together, 32 to a wave: a decode step of 8 heads a group fills 8 rows of one wave's products, a chunk of a prompt
 // fills workgroups of 128 rows.  The tile step is that of the sparse prefill: S^T = K Q^T, so that a lane owns a query row,
 // and O^T += V^T P^T in v_mfma_f32_32x32x16_bf16 with transposing LDS reads.  Two shapes of a workgroup (4 waves):
-//   few rows   one set of 32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory;
-//              one token of 32 heads at 128K keys (270 MB) 54 us, 5.0 TB/s
+//   few rows   32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory; one token
+//              of 32 heads at 128K keys (270 MB) 54 us, 5.0 TB/s
 //   many rows  each wave 32 of 128 rows, tiles of 64 keys shared by the four, K in codes for the 8-bit products.  Bound: matrix
 //              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 ms,
 //              1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
 // and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
-// launch.
+// launch (plan_of, at the end, says which shape and how many splits).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -229,7 +229,7 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
   }
 }
 
-// Few rows: one set of 32 query rows a workgroup, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers
+// Few rows: 32 query rows a workgroup, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers
 // on the way.  K and V become bf16 on their way into LDS, from registers that were read a tile ahead.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {

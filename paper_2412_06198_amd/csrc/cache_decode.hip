@@ -2,7 +2,8 @@
 // those of the step on bf16 tensors (decode.hip), half the bytes.  A key is read by 16 lanes as one 128-byte row
 // of codes of K and one of V and the two scales of its block.  s = scale_K (q . codes) and
 // p scale_V codes: the scales meet one number per key, not its elements.  The open block, at most 127 keys in bf16, has
-// a workgroup of its own.
+// a workgroup of its own.  The bound is a launch and the round trips to memory that follow one another: lists, keys,
+// partials, arrivals (8 heads at 4K tokens 6.7 us, as the step on bf16 tensors; 32 heads at 128K tokens, 3 % kept, 11.4, and 13.6 there).
 #include <algorithm>
 
 #include "cache_codes.h"

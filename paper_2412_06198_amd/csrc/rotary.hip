@@ -1,10 +1,10 @@
 // Rotary positions: pair i of a row at position p is turned by the angle p w_i,
 //   (x, y) -> (x cos - y sin, x sin + y cos).
 // Every element is read and written once and nothing else is: the bound is HBM (128K tokens of 40 heads 426 us, 6.3 TB/s
-// moved, where a device copy reaches 5.1), and the launch for a single token (2.2 us).  The sines and cosines of a token serve all heads of Q and K, so a thread takes
-// W pairs of one token and walks a range of heads with them in registers.  Angles are kept as fractions of a
-// turn in 64-bit fixed point: position times frequency modulo one turn is then one wrapping integer product,
-// exact for any position, where fp32 radians are off by a hundredth at 256K tokens.
+// moved, where a device copy reaches 5.1), and the launch for a single token (2.2 us).  The sines and cosines of a token
+// serve all heads of Q and K, so a thread takes W pairs of one token and walks a range of heads with them in registers.
+// Angles are kept as fractions of a turn in 64-bit fixed point: position times frequency modulo one turn is then one
+// wrapping integer product, exact for any position, where fp32 radians are off by a hundredth at 256K tokens.
 #include <algorithm>
 #include <cmath>
 #include <new>
