@@ -229,14 +229,18 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
   }
 }
 
-// Few rows: 32 query rows a workgroup, every wave its own keys, tiles of 32 of them in LDS of its own; no barriers
-// on the way.  K and V become bf16 on their way into LDS, from registers that were read a tile ahead.
+// Few rows: 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads half a row
+// of K, which it multiplies itself (the order of the elements of a product is free, Q has the same), and turns it into bf16 between the
+// products.  V becomes bf16 on its way into LDS, for the transposing reads.  Both are read a tile ahead.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
-  constexpr int NC = KT * 8 / 64;             // 16-byte pieces of codes of K, and of V, that a lane stages per tile
+  constexpr int NC = KT * 8 / 64;             // 16-byte pieces of codes of K, and of V, that a lane reads per tile
   constexpr int kMasked = 2;                  // tiles that some rows see and others do not, at most: 31 keys
-  __shared__ __attribute__((aligned(16))) uint16_t lds[WK][2][KT * 128];
+  __shared__ __attribute__((aligned(16))) union {
+    uint16_t v[WK][KT * 128];
+    float o[WK][32][kHeadDim];
+  } lds;
   __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles whose V has an infinity or NaN
   __shared__ float s_m[4][32], s_l[4][32];
 
@@ -255,15 +259,32 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   // this lane's row, and the last key that it sees
   const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
-  const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim;
-  const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim;
+  const uint8_t *__restrict__ Kh = p.K + (size_t)kvh * p.capacity * kHeadDim + q * kHeadDim + 64 * gg;
+  const uint8_t *__restrict__ Vh = p.V + (size_t)kvh * p.capacity * kHeadDim + lane * 16;
   const float *ksh = p.k_scale + (size_t)kvh * (p.capacity >> p.shift), *vsh = p.v_scale + (size_t)kvh * (p.capacity >> p.shift);
 
-  bf16x8 qf[8];  // Q^T fragments: B operand, lane = query row, 8 consecutive d per k-step half
+  uint4 kc[NC], vc[NC];
+  float ksc = 1.f, vsc = 1.f;
+  auto fetch_k = [&](int t) {
+    if (t >= min(t_end, n_closed)) return;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) kc[i] = *(const uint4 *)(Kh + (size_t)t * KT * kHeadDim + 16 * i);
+    ksc = ksh[(t * KT) >> p.shift];
+  };
+  auto fetch_v = [&](int t) {
+    if (t >= min(t_end, n_closed)) return;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) vc[i] = *(const uint4 *)(Vh + (size_t)t * KT * kHeadDim + 1024 * i);
+    vsc = vsh[(t * KT) >> p.shift];
+  };
+  fetch_k(t_begin + wave);
+  fetch_v(t_begin + wave);
+
+  bf16x8 qf[8];  // Q^T fragments: B operand, lane = query row, 8 consecutive d of the lane's half
   {
     const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 16 * ks + 8 * gg);
+    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 64 * gg + 8 * ks);
   }
   f32x16 oacc[4];
 #pragma unroll
@@ -273,94 +294,77 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   float m_run = -INFINITY;
   f32x4 lacc[2] = {};
 
-  // ---- staging: codes into registers, a tile ahead; then as bf16 into LDS ----------------------------
-  uint4 kc[NC], vc[NC];
-  float ksc = 1.f, vsc = 1.f;
-  auto fetch = [&](int t) {
-    if (t < n_closed) {
-      const size_t at = (size_t)t * KT * kHeadDim + lane * 16;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        kc[i] = *(const uint4 *)(Kh + at + (size_t)i * 1024);
-        vc[i] = *(const uint4 *)(Vh + at + (size_t)i * 1024);
-      }
-      const int blk = (t * KT) >> p.shift;
-      ksc = ksh[blk];
-      vsc = vsh[blk];
-    }
-  };
-  // LDS tiles are KT rows x 256 B, the 16-byte chunks of a row XOR-swizzled: K chunk c of row r at c ^ (r & 15) (b128
-  // reads of 16 rows hit 64 banks), V chunk c at c ^ ((r & 3) << 2) (the transposing b64 reads do).
-  auto put_keys = [&](uint16_t *tile, int r, int c16, int swz, const uint4 &lo, const uint4 &hi) {
-    char *at = (char *)tile + r * 256;
-    *(uint4 *)(at + (((2 * c16) ^ swz) << 4)) = lo;
-    *(uint4 *)(at + (((2 * c16 + 1) ^ swz) << 4)) = hi;
-  };
-  auto stage = [&](int t) {
-    const int j0 = t * KT;
-    const bool masked = t >= t_masked;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int id = lane + 64 * i, r = id >> 3, c16 = id & 7;
-      uint4 klo, khi, vlo, vhi;
-      if (t < n_closed) {
-        decode16<TYPE>(kc[i], ksc, klo, khi);
-        decode16<TYPE>(vc[i], vsc, vlo, vhi);
-      } else {  // the open block: bf16 rows, zeros behind the tokens
-        klo = khi = vlo = vhi = make_uint4(0u, 0u, 0u, 0u);
-        if (j0 + r < p.tokens) {
-          const size_t at = (((size_t)kvh << p.shift) + (size_t)(j0 + r - p.closed)) * kHeadDim + c16 * 16;
-          klo = *(const uint4 *)(p.k_open + at);
-          khi = *(const uint4 *)(p.k_open + at + 8);
-          vlo = *(const uint4 *)(p.v_open + at);
-          vhi = *(const uint4 *)(p.v_open + at + 8);
-        }
-      }
-      if (masked) {
-        // A row that does not see a key gives it weight 0, and 0 x inf is not 0: non-finite values of V
-        // stay out of the products here and come back at the end for the rows that do see them.
-        const uint32_t bad = nonfinite(vlo.x) | nonfinite(vlo.y) | nonfinite(vlo.z) | nonfinite(vlo.w) |
-                             nonfinite(vhi.x) | nonfinite(vhi.y) | nonfinite(vhi.z) | nonfinite(vhi.w);
-        const uint64_t who = __ballot(bad != 0u);
-        if (c16 == 0) rowbad[(t - t_masked) * KT + r] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
-        vlo = make_uint4(finite_only(vlo.x), finite_only(vlo.y), finite_only(vlo.z), finite_only(vlo.w));
-        vhi = make_uint4(finite_only(vhi.x), finite_only(vhi.y), finite_only(vhi.z), finite_only(vhi.w));
-      }
-      put_keys(lds[wave][0], r, c16, r & 15, klo, khi);
-      put_keys(lds[wave][1], r, c16, (r & 3) << 2, vlo, vhi);
-    }
-  };
-  const unsigned kbase = (unsigned)(q * 256) | (unsigned)((q & 15) << 4);
+  // LDS tiles are KT rows x 256 B, the 16-byte chunk c of row r at c ^ ((r & 3) << 2): transposing b64 reads hit 64 banks.
   unsigned vbase;
   {
     const int r = lane & 15, part = (lane >> 4) & 1, vrow = 4 * gg + (r >> 2);
     vbase = (unsigned)(vrow * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vrow & 3) << 2)) << 4) | (unsigned)((r & 1) << 3);
   }
-
-  auto attend = [&](int t) {
-    const int j0 = t * KT;
-    const uint16_t *Kt = lds[wave][0];
-    f32x16 sacc[1];  // S^T = K Q^T
-    bf16x8 kf[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) kf[i] = SA_KFRAG(Kt, 0, i);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const f32x16 zero = {};
-      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
-      if (i + 4 < 8) kf[i & 3] = SA_KFRAG(Kt, 0, i + 4);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    absorb_tile(sacc, j0 + KT - 1 > seen_all, see - j0 - 4 * gg, lds[wave][1], vbase, p.c, m_run, lacc, oacc);
+  auto put_v = [&](int i, int half, const uint4 &x) {  // 8 elements of piece i
+    const int r = (lane >> 3) + 8 * i, c = 2 * (lane & 7) + half;
+    *(uint4 *)((char *)lds.v[wave] + r * 256 + ((c ^ ((r & 3) << 2)) << 4)) = x;
   };
-
-  if (t_begin + wave < t_end) fetch(t_begin + wave);
   for (int t = t_begin + wave; t < t_end; t += WK) {
-    stage(t);
+    const int j0 = t * KT;
+    f32x16 sacc[1];  // S^T = K Q^T
+    auto multiply = [&](int i) {
+      const uint32_t c0 = i & 1 ? kc[i >> 1].z : kc[i >> 1].x, c1 = i & 1 ? kc[i >> 1].w : kc[i >> 1].y;
+      const u32x4 kf = {decode2<TYPE, false>(c0, ksc), decode2<TYPE, true>(c0, ksc), decode2<TYPE, false>(c1, ksc), decode2<TYPE, true>(c1, ksc)};
+      const f32x16 zero = {};
+      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
+    };
+    if (t < min(n_closed, t_masked)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // beside the products, V into LDS
+        multiply(i);
+        const uint32_t c0 = i & 1 ? vc[i >> 1].z : vc[i >> 1].x, c1 = i & 1 ? vc[i >> 1].w : vc[i >> 1].y;
+        put_v(i >> 1, i & 1, make_uint4(decode2<TYPE, false>(c0, vsc), decode2<TYPE, true>(c0, vsc), decode2<TYPE, false>(c1, vsc), decode2<TYPE, true>(c1, vsc)));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int r = (lane >> 3) + 8 * i;
+        uint4 lo, hi;
+        if (t < n_closed) {
+          decode16<TYPE>(vc[i], vsc, lo, hi);
+        } else {  // the open block: bf16 rows, zeros behind the tokens
+          lo = hi = make_uint4(0u, 0u, 0u, 0u);
+          if (j0 + r < p.tokens) {
+            const size_t at = (((size_t)kvh << p.shift) + (size_t)(j0 + r - p.closed)) * kHeadDim + (lane & 7) * 16;
+            lo = *(const uint4 *)(p.v_open + at);
+            hi = *(const uint4 *)(p.v_open + at + 8);
+          }
+        }
+        if (t >= t_masked) {
+          // A row that does not see a key gives it weight 0, and 0 x inf is not 0: non-finite values of V
+          // stay out of the products here and come back at the end for the rows that do see them.
+          const uint32_t bad = nonfinite(lo.x) | nonfinite(lo.y) | nonfinite(lo.z) | nonfinite(lo.w) |
+                               nonfinite(hi.x) | nonfinite(hi.y) | nonfinite(hi.z) | nonfinite(hi.w);
+          const uint64_t who = __ballot(bad != 0u);
+          if ((lane & 7) == 0) rowbad[(t - t_masked) * KT + r] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
+          lo = make_uint4(finite_only(lo.x), finite_only(lo.y), finite_only(lo.z), finite_only(lo.w));
+          hi = make_uint4(finite_only(hi.x), finite_only(hi.y), finite_only(hi.z), finite_only(hi.w));
+        }
+        put_v(i, 0, lo);
+        put_v(i, 1, hi);
+      }
+      if (t < n_closed) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) multiply(i);
+      } else {
+        const uint16_t *krow = p.k_open + (((size_t)kvh << p.shift) + (size_t)(min(j0 + q, p.tokens - 1) - p.closed)) * kHeadDim + 64 * gg;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // behind the tokens the last one again: not seen
+          const f32x16 zero = {};
+          sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(krow + 8 * i), qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
+        }
+      }
+    }
     wave_lds_sync();
-    if (t + WK < t_end) fetch(t + WK);
-    attend(t);
+    fetch_v(t + WK);
+    fetch_k(t + WK);
+    absorb_tile(sacc, j0 + KT - 1 > seen_all, see - j0 - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
     wave_lds_sync();
   }
   // Non-finite values of V in tiles that only some rows see: their share, for the rows that do.  Seldom there, so the
@@ -377,8 +381,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
 
   // ---- out: O / l in bf16, or the split's sums ------------------------------------------------------
   // the four waves' sums of the same rows, through the LDS of the tiles
-  float *const so = (float *)&lds[0][0][0];  // [4][32][128]
-  static_assert(sizeof(lds) >= 4 * 32 * 128 * 4, "holds the waves' outputs");
+  float *const so = &lds.o[0][0][0];
   __syncthreads();
   if (gg == 0) { s_m[wave][q] = m_run; s_l[wave][q] = l_run; }
 #pragma unroll
