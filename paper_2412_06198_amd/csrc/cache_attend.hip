@@ -776,16 +776,16 @@ size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 // Which kernel, and into how many splits the keys go.  Both are estimates of the same time, of terms that were each measured with
 // 32 heads over 300 to 130 thousand keys and 1 to 2000 tokens (us):
 //                                            few rows      many rows
-//   start and end                            5             7.3
+//   start and end                            5             7
 //   keys of a tile (few: of all four waves)  128           64
-//   a tile, up to a workgroup a compute unit 1.1           1.1
-//   a tile, two, which share it              1.95          1.3
+//   a tile, up to a workgroup a compute unit 0.75          1.15
+//   a tile, two, which share it              1.3           1.25
 //   start of the second one                  1             1
-//   a join: its launch 2.8, and 1 KB written and read for each row and split at 5 TB/s
+//   a join: its launch 3.4, and 1 KB written and read for each row and split at 4.3 TB/s
 // The least of them over no splits, as many as give one or two workgroups a compute unit, and in either range where the
-// join weighs as much as the tiles that it saves.  Over 384 shapes of 8 to 64 heads the choice is 1 % slower than the best of all
-// splits and kernels; fixed limits (600 thousand keys of all sets of 32 rows, 128 or 256 keys a split) were 3 %, and
-// at worst 11.7 us instead of 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6 (500 tokens of 64 heads at 1000).
+// join weighs as much as the tiles that it saves.  Over 379 shapes of 8 to 64 heads the choice is 1 % slower than the best of all
+// splits and both kernels; fixed limits on the keys read and the keys a split had been 3 %, and at worst 11.7 us instead of
+// 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6 (500 tokens of 64 heads at 1000).
 struct Plan { bool few; int S; };
 Plan plan_of(const Shape &sh, int rows, int tokens) {
   Plan best = {true, 1};
@@ -800,16 +800,16 @@ Plan plan_of(const Shape &sh, int rows, int tokens) {
       const int S0 = (int)std::max<int64_t>(1, std::min<int64_t>(splits, top));
       const int share = (tiles + S0 - 1) / S0, S = (tiles + share - 1) / share, per = (share + waves - 1) / waves;
       const float load = (float)wgs * S / sh.n_cu;
-      float t = few ? 5.f : 7.3f;
-      if (load <= 1.f) t += per * 1.1f;
-      else t += 1.f + per * (few ? 1.95f : 1.3f) * std::max(1.f, load / 2);
-      if (S > 1) t += 2.8f + all * S * 0.0002f;
+      float t = few ? 5.f : 7.f;
+      if (load <= 1.f) t += per * (few ? 0.75f : 1.15f);
+      else t += 1.f + per * (few ? 1.3f : 1.25f) * std::max(1.f, load / 2);
+      if (S > 1) t += 3.4f + all * S * 0.00023f;
       if (t < least) { least = t; best = {few != 0, S}; }
     };
     consider(1);
     for (int two = 0; two < 2; ++two) {
       const int64_t fill = (two + 1) * (int64_t)sh.n_cu / wgs;
-      const float even = std::sqrt((float)tiles / waves * (!two ? 1.1f : few ? 1.95f : 1.3f) / (all * 0.0002f));
+      const float even = std::sqrt((float)tiles / waves * (!few ? 1.2f : two ? 1.3f : 0.75f) / (all * 0.00023f));
       consider(fill);
       consider(std::min<int64_t>(fill, (int64_t)even));
     }
