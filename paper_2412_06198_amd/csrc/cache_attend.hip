@@ -6,7 +6,7 @@
 // fills workgroups of 128 rows.  The tile step is that of the sparse prefill: S^T = K Q^T, so that a lane owns a query row,
 // and O^T += V^T P^T in v_mfma_f32_32x32x16_bf16 with transposing LDS reads.  Two shapes of a workgroup (4 waves):
 //   few rows   32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory; one token
-//              of 32 heads at 128K keys (270 MB) 54 us, 5.0 TB/s
+//              of 32 heads at 128K keys (270 MB) 52 us, 5.2 TB/s
 //   many rows  each wave 32 of 128 rows, tiles of 64 keys shared by the four, K in codes for the 8-bit products.  Bound: matrix
 //              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 ms,
 //              1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
@@ -139,8 +139,6 @@ __device__ inline void put_row(const AttendArgs &p, int kvh, int row, int head, 
   }
 }
 
-#define SA_KFRAG(tile, hf, ks) \
-  (*(const bf16x8 *)((const char *)(tile) + ((kbase ^ (unsigned)((2 * (ks) + gg) << 4)) + (hf) * 32 * 256)))
 #define SA_VTR(tile, db, key0) \
   __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6)) + (key0) * 256)))
 
@@ -231,7 +229,8 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
 
 // Few rows: 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads half a row
 // of K, which it multiplies itself (the order of the elements of a product is free, Q has the same), and turns it into bf16 between the
-// products.  V becomes bf16 on its way into LDS, for the transposing reads.  Both are read a tile ahead.
+// products.  V becomes bf16 on its way into LDS, for the transposing reads.  Both are read a tile ahead.  (With K through LDS too, 250
+// tokens of 32 heads at 2200 keys took 27.8 us instead of 19.0, one at 128K 53.8 instead of 52.0.)
 template <int TYPE>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
