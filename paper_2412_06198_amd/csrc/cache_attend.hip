@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   int per = (n_tiles + p.S - 1) / p.S;
   if (per >= 64) per |= 1;  // 256 KB from workgroup to workgroup fall on few memory channels (130000 keys 60.3 us, odd 54.3)
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
-  const int n_closed = p.closed / KT;
+  const int t_full = min(t_end, p.closed / KT);  // tiles t_begin .. t_full - 1 are codes
 
   // this lane's row, and the last key that it sees
   const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
@@ -264,20 +264,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
 
   uint4 kc[NC], vc[NC];
   float ksc = 1.f, vsc = 1.f;
-  auto fetch_k = [&](int t) {
-    if (t >= min(t_end, n_closed)) return;
+  auto fetch = [&](int t) {
+    if (t >= t_full) return;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) kc[i] = *(const uint4 *)(Kh + (size_t)t * KT * kHeadDim + 16 * i);
+    for (int i = 0; i < NC; ++i) {
+      kc[i] = *(const uint4 *)(Kh + (size_t)t * KT * kHeadDim + 16 * i);
+      vc[i] = *(const uint4 *)(Vh + (size_t)t * KT * kHeadDim + 1024 * i);
+    }
     ksc = ksh[(t * KT) >> p.shift];
-  };
-  auto fetch_v = [&](int t) {
-    if (t >= min(t_end, n_closed)) return;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) vc[i] = *(const uint4 *)(Vh + (size_t)t * KT * kHeadDim + 1024 * i);
     vsc = vsh[(t * KT) >> p.shift];
   };
-  fetch_k(t_begin + wave);
-  fetch_v(t_begin + wave);
+  int t = t_begin + wave;
+  fetch(t);
 
   bf16x8 qf[8];  // Q^T fragments: B operand, lane = query row, 8 consecutive d of the lane's half
   {
@@ -303,68 +301,72 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
     const int r = (lane >> 3) + 8 * i, c = 2 * (lane & 7) + half;
     *(uint4 *)((char *)lds.v[wave] + r * 256 + ((c ^ ((r & 3) << 2)) << 4)) = x;
   };
-  for (int t = t_begin + wave; t < t_end; t += WK) {
-    const int j0 = t * KT;
-    f32x16 sacc[1];  // S^T = K Q^T
-    auto multiply = [&](int i) {
-      const uint32_t c0 = i & 1 ? kc[i >> 1].z : kc[i >> 1].x, c1 = i & 1 ? kc[i >> 1].w : kc[i >> 1].y;
-      const u32x4 kf = {decode2<TYPE, false>(c0, ksc), decode2<TYPE, true>(c0, ksc), decode2<TYPE, false>(c1, ksc), decode2<TYPE, true>(c1, ksc)};
-      const f32x16 zero = {};
-      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
-    };
-    if (t < min(n_closed, t_masked)) {
+  // A row that does not see a key gives it weight 0, and 0 x inf is not 0: in tiles that only some rows see, non-finite values
+  // of V stay out of the products and come back at the end for the rows that do see them.
+  auto mark = [&](int t, int i, bool bad) {
+    const uint64_t who = __ballot(bad);
+    if ((lane & 7) == 0) rowbad[(t - t_masked) * KT + (lane >> 3) + 8 * i] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
+    return who != 0ull;
+  };
+  auto absorb = [&](int t, f32x16 (&sacc)[1]) {
+    wave_lds_sync();
+    absorb_tile(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
+    wave_lds_sync();
+  };
+  for (; t < t_full; t += WK) {
+    if (t >= t_masked) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {  // beside the products, V into LDS
-        multiply(i);
-        const uint32_t c0 = i & 1 ? vc[i >> 1].z : vc[i >> 1].x, c1 = i & 1 ? vc[i >> 1].w : vc[i >> 1].y;
-        put_v(i >> 1, i & 1, make_uint4(decode2<TYPE, false>(c0, vsc), decode2<TYPE, true>(c0, vsc), decode2<TYPE, false>(c1, vsc), decode2<TYPE, true>(c1, vsc)));
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const int r = (lane >> 3) + 8 * i;
-        uint4 lo, hi;
-        if (t < n_closed) {
-          decode16<TYPE>(vc[i], vsc, lo, hi);
-        } else {  // the open block: bf16 rows, zeros behind the tokens
-          lo = hi = make_uint4(0u, 0u, 0u, 0u);
-          if (j0 + r < p.tokens) {
-            const size_t at = (((size_t)kvh << p.shift) + (size_t)(j0 + r - p.closed)) * kHeadDim + (lane & 7) * 16;
-            lo = *(const uint4 *)(p.v_open + at);
-            hi = *(const uint4 *)(p.v_open + at + 8);
-          }
-        }
-        if (t >= t_masked) {
-          // A row that does not see a key gives it weight 0, and 0 x inf is not 0: non-finite values of V
-          // stay out of the products here and come back at the end for the rows that do see them.
-          const uint32_t bad = nonfinite(lo.x) | nonfinite(lo.y) | nonfinite(lo.z) | nonfinite(lo.w) |
-                               nonfinite(hi.x) | nonfinite(hi.y) | nonfinite(hi.z) | nonfinite(hi.w);
-          const uint64_t who = __ballot(bad != 0u);
-          if ((lane & 7) == 0) rowbad[(t - t_masked) * KT + r] = ((who >> (lane & 56)) & 0xFFull) != 0ull;
-          lo = make_uint4(finite_only(lo.x), finite_only(lo.y), finite_only(lo.z), finite_only(lo.w));
-          hi = make_uint4(finite_only(hi.x), finite_only(hi.y), finite_only(hi.z), finite_only(hi.w));
-        }
-        put_v(i, 0, lo);
-        put_v(i, 1, hi);
-      }
-      if (t < n_closed) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) multiply(i);
-      } else {
-        const uint16_t *krow = p.k_open + (((size_t)kvh << p.shift) + (size_t)(min(j0 + q, p.tokens - 1) - p.closed)) * kHeadDim + 64 * gg;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {  // behind the tokens the last one again: not seen
-          const f32x16 zero = {};
-          sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(krow + 8 * i), qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
-        }
-      }
+      for (int i = 0; i < NC; ++i)
+        if (mark(t, i, (nonfinite_codes<TYPE>(vc[i].x) | nonfinite_codes<TYPE>(vc[i].y) | nonfinite_codes<TYPE>(vc[i].z) | nonfinite_codes<TYPE>(vc[i].w)) != 0u))
+          vc[i] = make_uint4(finite_codes<TYPE>(vc[i].x), finite_codes<TYPE>(vc[i].y), finite_codes<TYPE>(vc[i].z), finite_codes<TYPE>(vc[i].w));
     }
-    wave_lds_sync();
-    fetch_v(t + WK);
-    fetch_k(t + WK);
-    absorb_tile(sacc, j0 + KT - 1 > seen_all, see - j0 - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
-    wave_lds_sync();
+    f32x16 sacc[1];  // S^T = K Q^T
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {  // beside the products, V into LDS
+      auto words = [&](const uint4 &x, float scale) {
+        const uint32_t c0 = i & 1 ? x.z : x.x, c1 = i & 1 ? x.w : x.y;
+        return make_uint4(decode2<TYPE, false>(c0, scale), decode2<TYPE, true>(c0, scale), decode2<TYPE, false>(c1, scale), decode2<TYPE, true>(c1, scale));
+      };
+      const f32x16 zero = {};
+      const uint4 kf = words(kc[i >> 1], ksc);
+      const u32x4 kv = {kf.x, kf.y, kf.z, kf.w};
+      sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kv), qf[i], i == 0 ? zero : sacc[0], 0, 0, 0);
+      put_v(i >> 1, i & 1, words(vc[i >> 1], vsc));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    fetch(t + WK);
+    absorb(t, sacc);
+  }
+  // the open block: bf16 rows; behind the tokens the last one again, and zeros for V
+  for (; t < t_end; t += WK) {
+    const size_t first = (size_t)kvh << p.shift;
+    const uint16_t *krow = p.k_open + (first + (size_t)(min(t * KT + q, p.tokens - 1) - p.closed)) * kHeadDim + 64 * gg;
+    bf16x8 kf[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) kf[i] = *(const bf16x8 *)(krow + 8 * i);
+    uint4 lo[NC], hi[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const size_t at = (first + (size_t)(min(t * KT + (lane >> 3) + 8 * i, p.tokens - 1) - p.closed)) * kHeadDim + (lane & 7) * 16;
+      lo[i] = *(const uint4 *)(p.v_open + at);
+      hi[i] = *(const uint4 *)(p.v_open + at + 8);
+    }
+    f32x16 sacc[1] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], sacc[0], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      if (t * KT + (lane >> 3) + 8 * i >= p.tokens) lo[i] = hi[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (t >= t_masked &&
+          mark(t, i, (nonfinite(lo[i].x) | nonfinite(lo[i].y) | nonfinite(lo[i].z) | nonfinite(lo[i].w) |
+                      nonfinite(hi[i].x) | nonfinite(hi[i].y) | nonfinite(hi[i].z) | nonfinite(hi[i].w)) != 0u)) {
+        lo[i] = make_uint4(finite_only(lo[i].x), finite_only(lo[i].y), finite_only(lo[i].z), finite_only(lo[i].w));
+        hi[i] = make_uint4(finite_only(hi[i].x), finite_only(hi[i].y), finite_only(hi[i].z), finite_only(hi[i].w));
+      }
+      put_v(i, 0, lo[i]);
+      put_v(i, 1, hi[i]);
+    }
+    absorb(t, sacc);
   }
   // Non-finite values of V in tiles that only some rows see: their share, for the rows that do.  Seldom there, so the
   // scores are taken once more, plainly.
