@@ -250,8 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
   const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
   const int n_tiles = (p.pos + (min(r0 + kRowsFew, p.rows) - 1) / p.g) / KT + 1;
-  int per = (n_tiles + p.S - 1) / p.S;
-  if (per >= 64) per |= 1;  // 256 KB from workgroup to workgroup fall on few memory channels (130000 keys 60.3 us, odd 54.3)
+  const int per = (n_tiles + p.S - 1) / p.S;
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
   const int t_full = min(t_end, p.closed / KT);  // tiles t_begin .. t_full - 1 are codes
 
@@ -265,7 +264,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   uint4 kc[NC], vc[NC];
   float ksc = 1.f, vsc = 1.f;
   auto fetch = [&](int t) {
-    if (t >= t_full) return;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       kc[i] = *(const uint4 *)(Kh + (size_t)t * KT * kHeadDim + 16 * i);
@@ -274,8 +272,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
     ksc = ksh[(t * KT) >> p.shift];
     vsc = vsh[(t * KT) >> p.shift];
   };
-  int t = t_begin + wave;
-  fetch(t);
+  // A wave's tiles of codes are t_first and every fourth one, from a place on that puts the splits 512 KB / S apart modulo 512 KB:
+  // at the same distance of, say, 256 KB all of them ask the same few memory channels at a time (from the first tile on: one token at
+  // 130000 keys 60.3 us instead of 53.2, 16 tokens 84.9 instead of 67.6).
+  const int t_first = t_begin + wave, mine = max(0, (t_full - t_first + WK - 1) / WK);
+  int t = t_first;
+  if (mine > 0) t += ((sp * 128 / p.S - t_begin & 127) / WK) % mine * WK;
+  if (mine > 0) fetch(t);
 
   bf16x8 qf[8];  // Q^T fragments: B operand, lane = query row, 8 consecutive d of the lane's half
   {
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
     absorb_tile(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
     wave_lds_sync();
   };
-  for (; t < t_full; t += WK) {
+  for (int left = mine; left > 0; --left) {
     if (t >= t_masked) {
 #pragma unroll
       for (int i = 0; i < NC; ++i)
@@ -334,11 +337,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
       put_v(i >> 1, i & 1, words(vc[i >> 1], vsc));
       __builtin_amdgcn_sched_barrier(0);
     }
-    fetch(t + WK);
-    absorb(t, sacc);
+    const int now = t;
+    t = t + WK < t_full ? t + WK : t_first;
+    if (left > 1) fetch(t);
+    absorb(now, sacc);
   }
   // the open block: bf16 rows; behind the tokens the last one again, and zeros for V
-  for (; t < t_end; t += WK) {
+  for (t = t_first + mine * WK; t < t_end; t += WK) {
     const size_t first = (size_t)kvh << p.shift;
     const uint16_t *krow = p.k_open + (first + (size_t)(min(t * KT + q, p.tokens - 1) - p.closed)) * kHeadDim + 64 * gg;
     bf16x8 kf[8];
