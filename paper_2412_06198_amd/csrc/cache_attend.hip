@@ -44,7 +44,8 @@ struct AttendArgs {
   const uint16_t *k_open, *v_open;
   int64_t q_hs, q_rs, o_hs, o_rs, capacity;
   int g, Hkv, rows, tiles, S;  // query heads and query rows of a KV head, row tiles, splits of the keys
-  int turn;                    // row tiles from the last one down, this many, then from the first one up
+  int turn;                    // many rows: row tiles from the last one down, this many, then from the first one up; few: the first one
+                               // of those that go down, or 0
   int shift;                   // log2 of the block
   int pos, tokens, closed;     // of the first query; in the cache; in its full blocks
   float c;                     // softmax scale * log2(e)
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // KV heads side by side, then splits, then row tiles
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = rest / p.S * kRowsFew;
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = abs(p.turn - rest / p.S) * kRowsFew;
   const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
   const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
   const int n_tiles = (p.pos + (min(r0 + kRowsFew, p.rows) - 1) / p.g) / KT + 1;
@@ -787,13 +788,15 @@ size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 //   a tile, up to a workgroup a compute unit 0.75          1.15
 //   a tile, two, which share it              1.3           1.25
 //   start of the second one                  1             1
+//   more than two: their number times start and tiles, of which the rows see less than the longest one
 //   a join: its launch 3.4, and 1 KB written and read for each row and split at 4.3 TB/s
 // The least of them over no splits, as many as give one or two workgroups a compute unit, and in either range where the
 // join weighs as much as the tiles that it saves.  Over 379 shapes of 8 to 64 heads the choice is 1 % slower than the best of all
 // splits and both kernels; fixed limits on the keys read and the keys a split had been 3 %, and at worst 11.7 us instead of
 // 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6 (500 tokens of 64 heads at 1000).
 struct Plan { bool few; int S; };
-Plan plan_of(const Shape &sh, int rows, int tokens) {
+Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
+  const float mean = 0.5f + 0.5f * pos / tokens;  // keys that a row sees, against all
   Plan best = {true, 1};
   float least = INFINITY;
   const int64_t all = (int64_t)rows * sh.Hkv;
@@ -806,16 +809,15 @@ Plan plan_of(const Shape &sh, int rows, int tokens) {
       const int S0 = (int)std::max<int64_t>(1, std::min<int64_t>(splits, top));
       const int share = (tiles + S0 - 1) / S0, S = (tiles + share - 1) / share, per = (share + waves - 1) / waves;
       const float load = (float)wgs * S / sh.n_cu;
-      float t = few ? 5.f : 7.f;
-      if (load <= 1.f) t += per * (few ? 0.75f : 1.15f);
-      else t += 1.f + per * (few ? 1.3f : 1.25f) * std::max(1.f, load / 2);
+      const float start = few ? 5.f : 7.f, two = few ? 1.3f : 1.25f;
+      float t = load <= 1.f ? start + per * (few ? 0.75f : 1.15f) : 1.f + std::max(start + per * two, load / 2 * (start + per * two * mean));
       if (S > 1) t += 3.4f + all * S * 0.00023f;
       if (t < least) { least = t; best = {few != 0, S}; }
     };
     consider(1);
-    for (int two = 0; two < 2; ++two) {
-      const int64_t fill = (two + 1) * (int64_t)sh.n_cu / wgs;
-      const float even = std::sqrt((float)tiles / waves * (!few ? 1.2f : two ? 1.3f : 0.75f) / (all * 0.00023f));
+    for (int more = 0; more < 2; ++more) {
+      const int64_t fill = (more + 1) * (int64_t)sh.n_cu / wgs;
+      const float even = std::sqrt((float)tiles / waves * (!few ? 1.2f : more ? 1.3f : 0.75f) / (all * 0.00023f));
       consider(fill);
       consider(std::min<int64_t>(fill, (int64_t)even));
     }
@@ -839,13 +841,21 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   a.shift = sh.b == 128 ? 7 : 6;
   a.pos = pos; a.tokens = pos + n; a.closed = a.tokens >> a.shift << a.shift;
   a.c = sh.scale * 1.4426950408889634f;
-  const Plan plan = plan_of(sh, a.rows, a.tokens);
+  const Plan plan = plan_of(sh, a.rows, a.tokens, pos);
   a.tiles = (a.rows + (plan.few ? kRowsFew : kRowsMany) - 1) / (plan.few ? kRowsFew : kRowsMany);
   a.S = plan.S;
   const int64_t wgs = (int64_t)a.tiles * sh.Hkv, all = (int64_t)a.rows * sh.Hkv;
-  // Many rows: long row tiles first; where every compute unit gets one workgroup and some a second, the second ones in the
+  // Long row tiles first.  Many rows: where every compute unit gets one workgroup and some a second, the second ones in the
   // opposite order, so that the longest share theirs with the shortest (2048 tokens of 32 heads at 0: 49.2 -> 46.1 us, at 5K 178 -> 175).
-  a.turn = wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu ? std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S))) : a.tiles;
+  // Few rows: the short ones first where a round of one workgroup for most compute units is left at the end, which the long ones
+  // have for themselves (700 tokens of 32 heads at 700: 26.3 us, 30.0 the other way; 500 at 0, without such a round, 11.5 and 10.4).
+  a.turn = a.tiles;
+  if (plan.few) {
+    const int64_t left = wgs * a.S % (2 * sh.n_cu);
+    a.turn = 2 * left > sh.n_cu && left <= sh.n_cu ? 0 : a.tiles - 1;
+  } else if (wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu) {
+    a.turn = std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S)));
+  }
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
