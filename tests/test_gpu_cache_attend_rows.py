@@ -52,9 +52,9 @@ def _many(hq, hkv, n, tokens):
     return -(-(hq // hkv * n) // 32) * hkv * tokens > 600000 and hq // hkv * n > 32
 
 
-def _check(hq, hkv, b, n, pos, kind=sa.SA_CACHE_E4M3, seed=1, scale=0.0):
+def _check(hq, hkv, b, n, pos, kind=sa.SA_CACHE_E4M3, seed=1, scale=0.0, many=True):
     print(f"case rows hq={hq} hkv={hkv} b={b} n={n} pos={pos} kind={kind}", flush=True)
-    assert _many(hq, hkv, n, pos + n)
+    assert not many or _many(hq, hkv, n, pos + n)
     ses = sa.Session(hq, hkv, 4 * b, b, 32, keep=0.5, softmax_scale=scale)
     c, keys, vals, gen = _fill(ses, b, pos + n, kind, seed)
     q = torch.randn((hq, n, 128), generator=gen, device="cuda").bfloat16()
@@ -91,6 +91,13 @@ def test_a_workgroup_per_row_tile(pos):
 
 def test_many_row_tiles():
     _check(16, 2, 64, 5000, 700, seed=4)     # 626 workgroups
+
+
+@pytest.mark.parametrize("heads,n,pos", [((32, 8), 700, 0), ((32, 8), 700, 700), ((64, 8), 350, 0), ((24, 3), 1000, 500), ((24, 3), 700, 0),
+                                         ((32, 8), 500, 1500), ((8, 1), 4000, 0), ((5, 5), 1111, 3), ((128, 8), 200, 1)])
+def test_sets_of_32_rows_over_a_full_card(heads, n, pos):
+    # one to four workgroups of 32 rows a compute unit, from the longest row tile down or from the shortest up
+    _check(*heads, 64, n, pos, seed=13, many=False)
 
 
 def test_scale_of_the_softmax():
