@@ -8,8 +8,8 @@
 //   few rows   32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory; one token
 //              of 32 heads at 128K keys (270 MB) 52 us, 5.2 TB/s
 //   many rows  each wave 32 of 128 rows, tiles of 64 keys shared by the four, K in codes for the 8-bit products.  Bound: matrix
-//              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 ms,
-//              1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
+//              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 to 1.79 ms
+//              with the card, 1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
 // and the keys are split over workgroups where rows alone do not fill the card; the splits' sums are joined by a second
 // launch (plan_of, at the end, says which shape and how many splits).
 #include <algorithm>
