@@ -14,7 +14,6 @@
 // launch (plan_of, at the end, says which shape and how many splits).
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "cache_codes.h"
 #include "sa_internal.h"
