@@ -180,3 +180,34 @@ def test_refusals_of_the_session():
             call()
     ses.append(c, k, k, 0)
     torch.cuda.synchronize()
+
+
+def test_first_attend_inside_a_capture():
+    # the session's scratch is then allocated while recording, and serves eager calls after the graph is gone
+    print("case path first attend recorded", flush=True)
+    ses, other = (sa.Session(8, 2, 512, 64, 64, keep=0.3) for _ in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    K, V = (torch.randn((2, 5000, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    c = ses.cache(5056)
+    ses.append(c, K, V, 0)
+    q = torch.randn((8, 1, 128), generator=gen, device="cuda").bfloat16()
+    o, want = torch.empty_like(q), torch.empty_like(q)
+    other.attend(c, q, 4999, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        ses.attend(c, q, 4999, o)
+    for rep in range(3):
+        o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want), rep
+    del graph
+    torch.cuda.empty_cache()
+    filler = [torch.full((1 << 20,), 1e30, device="cuda") for _ in range(8)]
+    o.fill_(7.0)
+    ses.attend(c, q, 4999, o)
+    torch.cuda.synchronize()
+    assert torch.equal(o, want) and all((f == 1e30).all() for f in filler)
