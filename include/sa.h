@@ -348,6 +348,11 @@ sa_status sa_cache_decode(sa_ctx *ctx, const sa_cache *cache, const void *q, sa_
 sa_status sa_cache_attend_scratch_bytes(const sa_ctx *ctx, size_t *bytes);
 sa_status sa_cache_attend(sa_ctx *ctx, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
                           void *scratch_dev, size_t scratch_bytes, void *hip_stream);
+/* How such a call is carried out on the context's device, from the sizes alone (host only, nothing is launched): the query
+ * rows (a token's queries of one KV head are n_q_heads / n_kv_heads rows) that a workgroup takes, 32 or 128, of two
+ * kernels, and the number of workgroups that share the keys of a row, joined by a second launch if above 1.
+ * n >= 1, pos + n <= 2^30. */
+sa_status sa_cache_attend_plan(const sa_ctx *ctx, int64_t n, int64_t pos, int32_t *rows, int32_t *splits);
 
 const char *sa_last_error(const sa_ctx *ctx);
 

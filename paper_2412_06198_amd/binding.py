@@ -105,9 +105,10 @@ def library():
         lib.sa_cache_append.argtypes = [vp, C.POINTER(SaCache), SaRows, SaRows, C.c_int64, C.c_int64, vp]
         lib.sa_cache_decode.argtypes = [vp, C.POINTER(SaCache), vp, SaIndex, C.c_int64, vp, vp]
         lib.sa_cache_attend_scratch_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
+        lib.sa_cache_attend_plan.argtypes = [vp, C.c_int64, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         lib.sa_cache_attend.argtypes = [vp, C.POINTER(SaCache), SaRows, C.c_int64, C.c_int64, SaRows, vp, C.c_size_t, vp]
         for f in ("sa_rotary_create", "sa_rotary_embed", "sa_cache_bytes", "sa_cache_append", "sa_cache_decode",
-                  "sa_cache_attend_scratch_bytes", "sa_cache_attend"):
+                  "sa_cache_attend_scratch_bytes", "sa_cache_attend_plan", "sa_cache_attend"):
             getattr(lib, f).restype = st
         for f in ("sa_default_budgets", "sa_create", "sa_scores_bytes", "sa_index_bytes",
                   "sa_workspace_bytes", "sa_set_workspace", "sa_estimate_patterns",
@@ -278,6 +279,13 @@ def sa_cache_attend_scratch_bytes(ctx) -> int:
     out = C.c_size_t()
     _check(library().sa_cache_attend_scratch_bytes(ctx, C.byref(out)), ctx)
     return out.value
+
+
+def sa_cache_attend_plan(ctx, n, pos):
+    """(query rows of a workgroup, splits of the keys) of sa_cache_attend at these sizes."""
+    rows, splits = C.c_int32(), C.c_int32()
+    _check(library().sa_cache_attend_plan(ctx, n, pos, C.byref(rows), C.byref(splits)))
+    return rows.value, splits.value
 
 
 def sa_cache_attend(ctx, cache, Q: SaRows, n, pos, O: SaRows, scratch, scratch_bytes, stream=None):

@@ -460,11 +460,24 @@ sa_status sa_cache_attend_scratch_bytes(const sa_ctx *c, size_t *bytes) {
   return SA_OK;
 }
 
+// Whether n tokens of queries at pos are within the limits of a call.
+static bool attend_sizes(const sa_ctx *c, int64_t n, int64_t pos) {
+  return n >= 0 && pos >= 0 && n <= (int64_t)1 << 30 && pos <= (int64_t)1 << 30 && n * c->sh.Hq < (int64_t)1 << 30;
+}
+
+sa_status sa_cache_attend_plan(const sa_ctx *c, int64_t n, int64_t pos, int32_t *rows, int32_t *splits) {
+  if (!c || !rows || !splits || n == 0 || !attend_sizes(c, n, pos) || pos + n > (int64_t)1 << 30) return SA_ERR_INVALID_ARG;
+  int r, s;
+  sa::cache_attend_plan(c->sh, (int)n, (int)pos, &r, &s);
+  *rows = r;
+  *splits = s;
+  return SA_OK;
+}
+
 sa_status sa_cache_attend(sa_ctx *c, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
                           void *scratch, size_t scratch_bytes, void *stream) {
   if (!c) return SA_ERR_INVALID_ARG;
-  if (n < 0 || pos < 0 || n > (int64_t)1 << 30 || pos > (int64_t)1 << 30 || n * c->sh.Hq >= (int64_t)1 << 30)
-    return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
+  if (!attend_sizes(c, n, pos)) return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
   const sa_status s = check_cache(c, cache, pos + n);
   if (s != SA_OK) return s;
   if (!scratch || ((uintptr_t)scratch & 255)) return fail(c, SA_ERR_INVALID_ARG, "scratch must be a 256-byte aligned device pointer");

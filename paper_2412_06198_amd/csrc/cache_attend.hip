@@ -826,6 +826,12 @@ Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
 
 }  // namespace
 
+void cache_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits) {
+  const Plan plan = plan_of(sh, sh.g * n, pos + n, pos);
+  *rows = plan.few ? kRowsFew : kRowsMany;
+  *splits = plan.S;
+}
+
 size_t attend_scratch_bytes(const Shape &sh) { return max_slots(sh) * (kHeadDim * 4 + 8); }
 
 hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, int n, int pos, sa_rows O,

@@ -141,6 +141,7 @@ size_t cache_decode_partial_bytes(const Shape &sh);
 hipError_t launch_cache_decode(const Shape &sh, float *partials, const sa_cache &c, const uint16_t *q, sa_index idx,
                                int pos, uint16_t *o, hipStream_t st);
 size_t attend_scratch_bytes(const Shape &sh);
+void cache_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits);
 hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, int n, int pos, sa_rows O,
                                void *scratch, hipStream_t st);
 hipError_t launch_sparse_prefill(const Shape &sh, const Workspace &ws, const uint16_t *Q,
