@@ -515,12 +515,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
     fetch_v(t_begin);
     if (!open) issue_k(t_begin, 0);
   }
-  bf16x8 qf[8];  // Q^T fragments: B operand of the bf16 products, lane = row, 8 consecutive d per k-step half
-  {
-    const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 16 * ks + 8 * gg);
-  }
   f32x16 oacc[4];
 #pragma unroll
   for (int db = 0; db < 4; ++db)
@@ -534,51 +528,63 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
     vbase = (unsigned)(vr * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vr & 3) << 2)) << 4) | (unsigned)((r & 1) << 3);
   }
 
-  // ---- the open block first: its one or two tiles are bf16, their products too -----------------------------
-  for (int t = max(t_begin, n_closed); t < t_end; ++t) {
-    const int j0 = t * KT;
-    uint16_t *const Kt = (uint16_t *)&Ks[0][0];  // both buffers
-    __syncthreads();
+  // ---- tiles multiplied in bf16, with whole queries ---------------------------------------------------------
+  auto whole_tiles = [&](int from) {
+    if (from >= t_end) return;
+    bf16x8 qf[8];  // Q^T fragments: B operand, lane = row, 8 consecutive d per k-step half
+    const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int r = vrow + 32 * i, j = j0 + r;
-      uint4 x[4];
+    for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 16 * ks + 8 * gg);
+    for (int t = from; t < t_end; ++t) {
+      const int j0 = t * KT;
+      uint16_t *const Kt = (uint16_t *)&Ks[0][0];  // both buffers
+      __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (j < p.tokens) {  // zeros behind the tokens
-        const size_t at = (((size_t)kvh << p.shift) + (j - p.closed)) * kHeadDim + vch * 16;
-        x[0] = *(const uint4 *)(p.k_open + at);
-        x[1] = *(const uint4 *)(p.k_open + at + 8);
-        x[2] = *(const uint4 *)(p.v_open + at);
-        x[3] = *(const uint4 *)(p.v_open + at + 8);
-      }
-      if (t >= t_masked) {
-        uint32_t bad = 0u;
+      for (int i = 0; i < NC; ++i) {
+        const int r = vrow + 32 * i, j = j0 + r;
+        uint4 x[4];
 #pragma unroll
-        for (int k = 2; k < 4; ++k) {
-          bad |= nonfinite(x[k].x) | nonfinite(x[k].y) | nonfinite(x[k].z) | nonfinite(x[k].w);
-          x[k] = make_uint4(finite_only(x[k].x), finite_only(x[k].y), finite_only(x[k].z), finite_only(x[k].w));
+        for (int k = 0; k < 4; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (TYPE == SA_CACHE_E5M2 && j < p.closed) {
+          const size_t at = (size_t)j * kHeadDim + vch * 16;
+          decode16<TYPE>(*(const uint4 *)(Kh + at), ksh[j >> p.shift], x[0], x[1]);
+          decode16<TYPE>(*(const uint4 *)(Vh + at), vsh[j >> p.shift], x[2], x[3]);
+        } else if (j < p.tokens) {  // zeros behind the tokens
+          const size_t at = (((size_t)kvh << p.shift) + (j - p.closed)) * kHeadDim + vch * 16;
+          x[0] = *(const uint4 *)(p.k_open + at);
+          x[1] = *(const uint4 *)(p.k_open + at + 8);
+          x[2] = *(const uint4 *)(p.v_open + at);
+          x[3] = *(const uint4 *)(p.v_open + at + 8);
         }
-        mark(t, i, bad != 0u);
-      }
-      char *at = (char *)Kt + r * 256;  // chunk c of row r at c ^ (r & 15)
-      *(uint4 *)(at + (((2 * vch) ^ (r & 15)) << 4)) = x[0];
-      *(uint4 *)(at + (((2 * vch + 1) ^ (r & 15)) << 4)) = x[1];
-      put_v(1, i, x[2], x[3]);
-    }
-    __syncthreads();
-    if (j0 <= see1) {
-      f32x16 sacc[2] = {};
+        if (t >= t_masked) {
+          uint32_t bad = 0u;
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const bf16x8 kf = *(const bf16x8 *)((const char *)Kt + (32 * hf + q) * 256 + (((2 * ks + gg) ^ (q & 15)) << 4));
-          sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sacc[hf], 0, 0, 0);
+          for (int k = 2; k < 4; ++k) {
+            bad |= nonfinite(x[k].x) | nonfinite(x[k].y) | nonfinite(x[k].z) | nonfinite(x[k].w);
+            x[k] = make_uint4(finite_only(x[k].x), finite_only(x[k].y), finite_only(x[k].z), finite_only(x[k].w));
+          }
+          mark(t, i, bad != 0u);
         }
-      absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[1], vbase, p.c, m_run, lacc, oacc);
+        char *at = (char *)Kt + r * 256;  // chunk c of row r at c ^ (r & 15)
+        *(uint4 *)(at + (((2 * vch) ^ (r & 15)) << 4)) = x[0];
+        *(uint4 *)(at + (((2 * vch + 1) ^ (r & 15)) << 4)) = x[1];
+        put_v(1, i, x[2], x[3]);
+      }
+      __syncthreads();
+      if (j0 <= see1) {
+        f32x16 sacc[2] = {};
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const bf16x8 kf = *(const bf16x8 *)((const char *)Kt + (32 * hf + q) * 256 + (((2 * ks + gg) ^ (q & 15)) << 4));
+            sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sacc[hf], 0, 0, 0);
+          }
+        absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[1], vbase, p.c, m_run, lacc, oacc);
+      }
     }
-  }
+  };
+  whole_tiles(max(t_begin, n_closed));  // the open block first
   if (open && t_begin < t_full) {
     __syncthreads();
     issue_k(t_begin, 0);
@@ -687,6 +693,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
         vsc = uniform_load(vsh, ((t + 2) * KT) >> p.shift);
       }
       if (j0 <= see1) absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[cur], vbase, p.c, m_run, lacc, oacc);
+    }
+  }
+
+  // An infinite key (e5m2 has them) times the two codes of a query's element is inf * 0 or inf - inf where the score is -inf and
+  // its key weighs nothing.  Like any NaN that stays in the row's sum, so where there is one the workgroup starts anew, with
+  // whole queries for all its tiles (seldom; looking for infinities in the loop would cost every call).
+  if (TYPE == SA_CACHE_E5M2 && t_begin < t_full) {
+    const float l = lacc[0][0] + lacc[1][0];
+    if (__syncthreads_or(l != l)) {
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+      m_run = -INFINITY;
+      lacc[0] = lacc[1] = f32x4{};
+      whole_tiles(t_begin);
     }
   }
 
