@@ -144,7 +144,10 @@ __device__ inline void put_row(const AttendArgs &p, int kvh, int row, int head, 
 
 // A tile's scores (lane = row, accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4 of HF * 32) into a row's running
 // softmax and its outputs.  masked: keys from place lim + 1 (less 4gg) on are not seen.
-template <int HF>
+// PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each, which adds to an output as much error as
+// its own rounding does (0.0023 of the outputs' scale, rounding alone 0.0017).  2: a leading part and the rest, 2^-15, by twice
+// the products: 0.0017.  launch_cache_attend says which.
+template <int PARTS, int HF>
 __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, const uint16_t *Vt, unsigned vbase, float c,
                                    float &m_run, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -181,12 +184,23 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
     for (int e = 2 * j; e < 2 * j + 2; ++e)
       sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[g >> 1][8 * (g & 1) + e], c, -m_ref));
   };
-  u32x4 pbuf[2];
+  u32x4 pbuf[2][PARTS];
   auto cvt2 = [&](int g, int j) {
-    const bf16x2 pr = {(__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j], (__bf16)sacc[g >> 1][8 * (g & 1) + 2 * j + 1]};
-    pbuf[g & 1][j] = __builtin_bit_cast(uint32_t, pr);
+    const float a = sacc[g >> 1][8 * (g & 1) + 2 * j], b = sacc[g >> 1][8 * (g & 1) + 2 * j + 1];
+    if constexpr (PARTS == 1) {
+      const bf16x2 pr = {(__bf16)a, (__bf16)b};
+      pbuf[g & 1][0][j] = __builtin_bit_cast(uint32_t, pr);
+    } else {
+      // The leading part is cut, not rounded, and the rest taken from p (1 + 2^-20), which the normaliser sees too: neither
+      // part is negative, nor 0 before p is below 2^-113, so that an infinite V stays infinite.
+      const uint32_t wa = __float_as_uint(a), wb = __float_as_uint(b);
+      const bf16x2 rest = {(__bf16)__builtin_fmaf(a, 1.f + 0x1p-20f, -__uint_as_float(wa & 0xFFFF0000u)),
+                           (__bf16)__builtin_fmaf(b, 1.f + 0x1p-20f, -__uint_as_float(wb & 0xFFFF0000u))};
+      pbuf[g & 1][0][j] = __builtin_amdgcn_perm(wb, wa, 0x07060302u);
+      pbuf[g & 1][1][j] = __builtin_bit_cast(uint32_t, rest);
+    }
   };
-  // The normaliser sums the probabilities as rounded to bf16, so that a row stays a convex combination of its V rows;
+  // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
   // 4x4x4 products with ones do it on the matrix pipe.
   const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
   s16x4 vlo[4], vhi[4];
@@ -205,16 +219,20 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
     const int g = i >> 2, db = i & 3;
     if (db == 0) {
       cvt2(g, 3);
-      asm("" : "+v"(pbuf[g & 1]));
+#pragma unroll
+      for (int x = 0; x < PARTS; ++x) asm("" : "+v"(pbuf[g & 1][x]));
     }
-    const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1]);
     const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
-    oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
-    const s16x8 ps = __builtin_bit_cast(s16x8, pb);
-    if (db == 0)
-      lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
-    if (db == 3)
-      lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) {
+      const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1][x]);
+      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
+      const s16x8 ps = __builtin_bit_cast(s16x8, pb);
+      if (db == 0)
+        lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+      if (db == 3)
+        lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+    }
     if (i + 4 < 8 * HF) {
       vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
       vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
@@ -231,7 +249,7 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
 // of K, which it multiplies itself (the order of the elements of a product is free, Q has the same), and turns it into bf16 between the
 // products.  V becomes bf16 on its way into LDS, for the transposing reads.  Both are read a tile ahead.  (With K through LDS too, 250
 // tokens of 32 heads at 2200 keys took 27.8 us instead of 19.0, one at 128K 53.8 instead of 52.0.)
-template <int TYPE>
+template <int TYPE, int PARTS>
 __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
   constexpr int NC = KT * 8 / 64;             // 16-byte pieces of codes of K, and of V, that a lane reads per tile
@@ -313,7 +331,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
   };
   auto absorb = [&](int t, f32x16 (&sacc)[1]) {
     wave_lds_sync();
-    absorb_tile(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
+    absorb_tile<PARTS>(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
     wave_lds_sync();
   };
   for (int left = mine; left > 0; --left) {
@@ -580,7 +598,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
             const bf16x8 kf = *(const bf16x8 *)((const char *)Kt + (32 * hf + q) * 256 + (((2 * ks + gg) ^ (q & 15)) << 4));
             sacc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sacc[hf], 0, 0, 0);
           }
-        absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[1], vbase, p.c, m_run, lacc, oacc);
+        absorb_tile<1>(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[1], vbase, p.c, m_run, lacc, oacc);
       }
     }
   };
@@ -692,7 +710,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs p) 
         fetch_v(t + 2);
         vsc = uniform_load(vsh, ((t + 2) * KT) >> p.shift);
       }
-      if (j0 <= see1) absorb_tile(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[cur], vbase, p.c, m_run, lacc, oacc);
+      if (j0 <= see1) absorb_tile<1>(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[cur], vbase, p.c, m_run, lacc, oacc);
     }
   }
 
@@ -887,9 +905,16 @@ hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, in
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
   const bool e4m3 = c.type == SA_CACHE_E4M3;
-  if (plan.few) {
-    if (e4m3) attend_few_kernel<SA_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
-    else attend_few_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
+  // Probabilities in two parts where a key is read for one or two sets of 32 rows, steps and drafted tokens, which wait for memory or
+  // for the launch (32 heads: one token at 128K keys 53.7 us instead of 53.4, at 10K 10.9 and 10.6, at 500 8.3 and 7.7, 16 tokens at 16K 16.3
+  // and 15.5).  Chunks of a prompt, bound by the products, take them in bf16 as the sparse prefill does: with two parts 250 tokens at
+  // 2200 keys take 21.8 us instead of 18.8, 2048 at 64K in the other kernel 2516 instead of 1652.
+  if (plan.few && a.rows <= 2 * kRowsFew) {
+    if (e4m3) attend_few_kernel<SA_CACHE_E4M3, 2><<<grid, kThreads, 0, st>>>(a);
+    else attend_few_kernel<SA_CACHE_E5M2, 2><<<grid, kThreads, 0, st>>>(a);
+  } else if (plan.few) {
+    if (e4m3) attend_few_kernel<SA_CACHE_E4M3, 1><<<grid, kThreads, 0, st>>>(a);
+    else attend_few_kernel<SA_CACHE_E5M2, 1><<<grid, kThreads, 0, st>>>(a);
   } else {
     if (e4m3) attend_rows_kernel<SA_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
     else attend_rows_kernel<SA_CACHE_E5M2><<<grid, kThreads, 0, st>>>(a);
