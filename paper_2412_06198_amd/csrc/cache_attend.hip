@@ -454,8 +454,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
 //   K stays in codes: they go from memory into LDS as they are (the LDS DMA, no registers) and into the 8-bit matrix
 //   instructions, at twice the rate of the bf16 ones.  Q, in bf16, is cut into two codes of e4m3, q = hi + lo: hi is q
 //   rounded to 4 significant bits, and what is left fits 4 more, exactly, so that two products at twice the rate
-//   multiply all of q (an element below 2^-14 of its row's largest loses bits that are below 2^-23 of that one).  The scales of
-//   Q's rows and of the block of K are exponents that the instruction takes.
+//   multiply all of q.  (The largest element of a row lies in (224, 448] scales; one below 2^-6 scales is rounded to a 16th of the
+//   least code: off by 2^-14 scales, 2^-21.8 of the row's largest, at most.)  The scales of Q's rows and of the block of K are
+//   exponents that the instruction takes.
 //   V has to be multiplied with probabilities, which need bf16: its codes are turned into bf16 on their way into LDS, from
 //   registers that were read a tile ahead.
 template <int TYPE>
