@@ -298,7 +298,7 @@ void sa_rotary_destroy(sa_rotary *rotary);
 /* Row t of every head of Q [n_q_heads][n] and K [n_kv_heads][n] turned to position pos + t, or to
  * positions[t] (DEVICE int32[n]; negative ones and repeats are fine; then pos is not used):
  *   pair (x, y) -> (x cos - y sin, x sin + y cos) * amplitude at angle position * w_i.
- * Angles are exact to 2^-32 of a turn at any position; the arithmetic is fp32, rounded to bf16 once.
+ * Angles are off by less than 2^-25 of a turn at any position; the arithmetic is fp32, rounded to bf16 once.
  * Q_out may be Q with the same strides (in place), likewise K_out; other overlaps are not allowed.
  * Q.data or K.data may be NULL: that side is left out.  n <= 2^25, 0 <= pos, pos + n <= 2^31; n = 0 does nothing. */
 sa_status sa_rotary_embed(sa_ctx *ctx, const sa_rotary *rotary, sa_rows Q, sa_rows K, int64_t n, int64_t pos,

@@ -6,7 +6,7 @@
 // fills workgroups of 128 rows.  The tile step is that of the sparse prefill: S^T = K Q^T, so that a lane owns a query row,
 // and O^T += V^T P^T in v_mfma_f32_32x32x16_bf16 with transposing LDS reads.  Two shapes of a workgroup (4 waves):
 //   few rows   32 rows, each wave every fourth tile of 32 keys, in LDS of its own, no barriers.  Bound: memory; one token
-//              of 32 heads at 128K keys (270 MB) 52 us, 5.2 TB/s
+//              of 32 heads at 128K keys (270 MB) 53.5 us, 5.0 TB/s
 //   many rows  each wave 32 of 128 rows, tiles of 64 keys shared by the four, K in codes for the 8-bit products.  Bound: matrix
 //              pipe, busy 65 % of the time, at the 2.0 GHz that the power limit leaves: 2048 tokens at 64K keys 1.70 to 1.79 ms
 //              with the card, 1.27 PFLOP/s, where a large bf16 product of the library reaches 1.32
@@ -454,8 +454,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few_kernel(AttendArgs p) {
 //   K stays in codes: they go from memory into LDS as they are (the LDS DMA, no registers) and into the 8-bit matrix
 //   instructions, at twice the rate of the bf16 ones.  Q, in bf16, is cut into two codes of e4m3, q = hi + lo: hi is q
 //   rounded to 4 significant bits, and what is left fits 4 more, exactly, so that two products at twice the rate
-//   multiply all of q.  (The largest element of a row lies in (224, 448] scales; one below 2^-6 scales is rounded to a 16th of the
-//   least code: off by 2^-14 scales, 2^-21.8 of the row's largest, at most.)  The scales of Q's rows and of the block of K are
+//   multiply all of q.  (The largest element of a row, if 2^-92 or more, lies in (224, 448] scales; one below 2^-6 scales is rounded to a
+//   16th of the least code: off by 2^-14 scales, 2^-21.8 of the row's largest, at most.)  The scales of Q's rows and of the block of K are
 //   exponents that the instruction takes.
 //   V has to be multiplied with probabilities, which need bf16: its codes are turned into bf16 on their way into LDS, from
 //   registers that were read a tile ahead.
@@ -820,8 +820,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs p) {
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit.
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 
-// Which kernel, and into how many splits the keys go.  Both are estimates of the same time, of terms that were each measured with
-// 32 heads over 300 to 130 thousand keys and 1 to 2000 tokens (us):
+// Which kernel, and into how many splits the keys go: what orders them is a sum of terms that were each measured with
+// 32 heads over 300 to 130 thousand keys and 1 to 2000 tokens (us).  It has no term for the rate of memory or the power limit, so
+// for the longest calls it is less than the time (32 for one token of 32 heads at 128K keys, which takes 53).
 //                                            few rows      many rows
 //   start and end                            5             7
 //   keys of a tile (few: of all four waves)  128           64
@@ -831,9 +832,10 @@ size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 //   more than two: their number times start and tiles, of which the rows see less than the longest one
 //   a join: its launch 3.4, and 1 KB written and read for each row and split at 4.3 TB/s
 // The least of them over no splits, as many as give one or two workgroups a compute unit, and in either range where the
-// join weighs as much as the tiles that it saves.  Over 379 shapes of 8 to 64 heads the choice is 1 % slower than the best of all
-// splits and both kernels; fixed limits on the keys read and the keys a split had been 3 %, and at worst 11.7 us instead of
-// 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6 (500 tokens of 64 heads at 1000).
+// join weighs as much as the tiles that it saves.  Over 170 drawn shapes of 8 to 64 heads the choice is 1.7 % slower than the best of
+// both kernels and all splits in the mean, 27 % at worst (9 tokens of 16 heads at 110648 keys, 40.5 us: half the splits 31.9); fixed
+// limits on the keys read and the keys a split had been 11.7 us instead of 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6
+// (500 tokens of 64 heads at 1000).
 struct Plan { bool few; int S; };
 Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
   const float mean = 0.5f + 0.5f * pos / tokens;  // keys that a row sees, against all

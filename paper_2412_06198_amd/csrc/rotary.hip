@@ -1,10 +1,11 @@
 // Rotary positions: pair i of a row at position p is turned by the angle p w_i,
 //   (x, y) -> (x cos - y sin, x sin + y cos).
-// Every element is read and written once and nothing else is: the bound is HBM (128K tokens of 40 heads 426 us, 6.3 TB/s
-// moved, where a device copy reaches 5.1), and the launch for a single token (2.2 us).  The sines and cosines of a token
+// Every element is read and written once and nothing else is: the bound is HBM (128K tokens of 40 heads 446 us, 6.0 TB/s
+// moved, where a device copy reaches 5.1; 429 in a replayed loop), and the launch for a single token (2.2 us).  The sines and cosines of a token
 // serve all heads of Q and K, so a thread takes W pairs of one token and walks a range of heads with them in registers.
 // Angles are kept as fractions of a turn in 64-bit fixed point: position times frequency modulo one turn is then one
-// wrapping integer product, exact for any position, where fp32 radians are off by a hundredth at 256K tokens.
+// wrapping integer product, to 2^-32 of a turn for any position, where fp32 radians are off by a hundredth at 256K tokens.  As an
+// fp32 number, 24 bits of half a turn, it is off by 2^-26 of a turn more at most.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -183,8 +184,8 @@ hipError_t launch_rotary(const Shape &sh, const RotaryTable &f, sa_rows Q, sa_ro
   const int w = most >= 4 && f.pairs % 4 == 0 ? 4 : f.pairs % 2 == 0 ? 2 : 1;
   const int64_t tiles = (n + kThreads * w / 64 - 1) / (kThreads * w / 64);
   // Heads of a thread: as many as leave eight workgroups a compute unit, but three at most.  With more the workgroups, which
-  // drift apart, have every head's memory open at once: 128K tokens of 40 heads (2.68 GB) 426 us, 6.3 TB/s, with 3 heads, 520 with
-  // 16 and 540 with all 40; one head each costs the sines, 570.
+  // drift apart, have every head's memory open at once: 128K tokens of 40 heads (2.68 GB) in a replayed loop 429 us with 3 heads,
+  // 479 with 16 and 508 with all 40; one head each costs the sines, 555.
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>(a.H, 8 * (int64_t)sh.n_cu / tiles));
   a.per = std::min((int)((a.H + want - 1) / want), 3);
   const dim3 grid((unsigned)tiles, (unsigned)((a.H + a.per - 1) / a.per));
