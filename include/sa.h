@@ -330,7 +330,10 @@ sa_status sa_cache_bytes(const sa_ctx *ctx, int64_t capacity, size_t sizes[6]);
  * the type), 1 if all its values are 0, and the codes nearest to value / s (ties to even): the bytes depend on
  * the block's values alone, not on how many calls brought them.  NaN stays NaN; an infinity becomes NaN in
  * e4m3, which has none.  n <= 2^25, pos + n <= capacity; n = 0 does nothing.  The earlier rows of the open block are read
- * from k_open, v_open, so pos can be taken back inside the open block, but not into a full one. */
+ * from k_open, v_open, so pos can be taken back inside the open block, but not into a full one: the call that fills a
+ * block may write over its rows there.  A caller who may take tokens back across it (drafted ones that are rejected)
+ * copies k_open and v_open before that call and, to take them back, puts the copies there and appends again from that
+ * call's pos on, or from an earlier one inside the same block; nothing else has to be restored. */
 sa_status sa_cache_append(sa_ctx *ctx, const sa_cache *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos,
                           void *hip_stream);
 

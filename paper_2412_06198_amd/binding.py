@@ -502,7 +502,8 @@ class Session:
         return cache.struct()
 
     def append(self, cache, K, V, pos):
-        """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds."""
+        """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds.  To take tokens back across a block that a call
+        has filled: copies of cache.k_open and cache.v_open from before it, put back, and append() again from its pos on."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
