@@ -490,7 +490,7 @@ class Session:
         sizes = sa_cache_bytes(self.ctx, capacity)
         h, b, t = self.cfg.n_kv_heads, self.cfg.block, self.torch
         kinds = [((h, capacity, 128), t.uint8)] * 2 + [((h, capacity // b), t.float32)] * 2 + [((h, b, 128), t.bfloat16)] * 2
-        bufs = [t.empty(shape, dtype=kind, device=self.device) for shape, kind in kinds]
+        bufs = [t.empty(shape, dtype=kind, device=self.ws.device) for shape, kind in kinds]  # self.device may have no index
         assert [x.nbytes for x in bufs] == sizes
         return Cache(*bufs, cache_type)
 
@@ -532,7 +532,7 @@ class Session:
         replays of graphs on several streams among them, need sessions of their own."""
         if self._attend_scratch is None:
             size = sa_cache_attend_scratch_bytes(self.ctx)
-            raw = self.torch.empty(size + 256, dtype=self.torch.uint8, device=self.device)
+            raw = self.torch.empty(size + 256, dtype=self.torch.uint8, device=self.ws.device)
             off = (-raw.data_ptr()) % 256
             self._attend_scratch = (raw, raw.data_ptr() + off, size)
         return self._attend_scratch
