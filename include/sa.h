@@ -245,8 +245,8 @@ sa_status sa_search_patterns(sa_ctx *ctx, const void *Q, const void *K, const vo
 /* ---- rotary positions, and the cache in 8 bits ---------------------------------------------------
  * Calls that take a number of tokens of their own take their tensors as sa_rows: a DEVICE tensor
  * [heads][n][128] of bf16, its 128 elements adjacent, strides in elements, 0 for both =>
- * contiguous.  The address must be 16-byte aligned, strides positive multiples of 8; any order of heads and
- * rows will do.  The rows of an output must not overlap one another.  Token numbers (n, pos) are host values: a call
+ * contiguous.  The address must be 16-byte aligned, strides multiples of 8 and at least 128 (the stride of a single
+ * head or row does not matter); any order of heads and rows will do.  The rows of an output must not overlap one another.  Token numbers (n, pos) are host values: a call
  * recorded into a graph repeats them.  These calls run on the current
  * device, which must be the one of the stream and of every pointer, and need no workspace unless they say so. */
 typedef struct {
@@ -338,14 +338,17 @@ sa_status sa_cache_append(sa_ctx *ctx, const sa_cache *cache, sa_rows K, sa_rows
                           void *hip_stream);
 
 /* sa_sparse_decode on a cache that holds tokens 0 .. pos: same index, same kept keys, same q, o and pos, same
- * use of ctx's workspace.  ctx's strides of K and V do not matter. */
+ * use of ctx's workspace.  ctx's strides of K and V do not matter.  NaN among the scores of kept keys gives NaN, as in
+ * sa_cache_attend; sa_sparse_decode gives 0 to a head whose scores are all NaN. */
 sa_status sa_cache_decode(sa_ctx *ctx, const sa_cache *cache, const void *q, sa_index idx, int64_t pos, void *o,
                           void *hip_stream);
 
 /* Causal attention of the newest n tokens of a cache that holds pos + n: the query of row t of Q
  * [n_q_heads][n] attends tokens 0 .. pos + t, with the prefill's scaled softmax.  n from 1 (a decode step without
  * an index) over a handful of drafted tokens to chunks of a prompt; n * n_q_heads < 2^30.  O may be Q with the
- * same strides.
+ * same strides.  Scores, sums and statistics are fp32 and the output is rounded to bf16 once; probabilities are multiplied
+ * to 2^-15 of themselves, but rounded to bf16, as in the prefill, with more than 64 query rows a KV head (n * n_q_heads /
+ * n_kv_heads) or where sa_cache_attend_plan says 128 rows.
  * scratch: DEVICE, 256-byte aligned, sa_cache_attend_scratch_bytes bytes (the same for every n and pos; calls
  * that may overlap in time need one each, as replays of captured graphs on several streams do). */
 sa_status sa_cache_attend_scratch_bytes(const sa_ctx *ctx, size_t *bytes);

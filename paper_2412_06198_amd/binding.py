@@ -538,7 +538,8 @@ class Session:
         return self._attend_scratch
 
     def attend(self, cache, Q, pos, O):
-        """Causal attention of the newest tokens, Q and O [n_q_heads, n, 128], over a cache that holds pos + n."""
+        """Causal attention of the newest tokens, Q and O [n_q_heads, n, 128], over a cache that holds pos + n.  Partial results
+        go through the session's one scratch, see attend_scratch(): calls that may overlap in time need sessions of their own."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
