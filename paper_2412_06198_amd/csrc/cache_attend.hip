@@ -192,7 +192,7 @@ __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, con
       pbuf[g & 1][0][j] = __builtin_bit_cast(uint32_t, pr);
     } else {
       // The leading part is cut, not rounded, and the rest taken from p (1 + 2^-20), which the normaliser sees too: neither
-      // part is negative, nor 0 before p is below 2^-113, so that an infinite V stays infinite.
+      // part is negative, nor 0 or subnormal before p is below 2^-106, so that an infinite V stays infinite.
       const uint32_t wa = __float_as_uint(a), wb = __float_as_uint(b);
       const bf16x2 rest = {(__bf16)__builtin_fmaf(a, 1.f + 0x1p-20f, -__uint_as_float(wa & 0xFFFF0000u)),
                            (__bf16)__builtin_fmaf(b, 1.f + 0x1p-20f, -__uint_as_float(wb & 0xFFFF0000u))};
