@@ -832,7 +832,7 @@ size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 2 * kRowsMany; }
 //   more than two: their number times start and tiles, of which the rows see less than the longest one
 //   a join: its launch 3.4, and 1 KB written and read for each row and split at 4.3 TB/s
 // The least of them over no splits, as many as give one or two workgroups a compute unit, and in either range where the
-// join weighs as much as the tiles that it saves.  Over 170 drawn shapes of 8 to 64 heads the choice is 1.7 % slower than the best of
+// join weighs as much as the tiles that it saves.  Over 169 drawn shapes of 8 to 64 heads the choice is 1.6 % slower than the best of
 // both kernels and all splits in the mean, 27 % at worst (9 tokens of 16 heads at 110648 keys, 40.5 us: half the splits 31.9); fixed
 // limits on the keys read and the keys a split had been 11.7 us instead of 8.8 (130 tokens at 260 keys), 37.7 instead of 27.6
 // (500 tokens of 64 heads at 1000).
