@@ -13,7 +13,8 @@
  * pattern search (sa_search_patterns); rotary positions of Q and K in front of it
  * (sa_rotary_embed); and behind it a cache that holds K and V in 8 bits
  * (sa_cache_append) with the decode step over the index (sa_cache_decode) and causal
- * attention of the newest tokens (sa_cache_attend) that read it.
+ * attention of the newest tokens (sa_cache_attend) that read it, or back to bf16
+ * (sa_cache_read); and the same four over a cache in 4 bits (sa_cache4_*).
  *
  * Conventions
  *   - C99 types only.  Q, K, V, O are DEVICE pointers to raw bf16 (16-bit)
@@ -359,6 +360,48 @@ sa_status sa_cache_attend(sa_ctx *ctx, const sa_cache *cache, sa_rows Q, int64_t
  * kernels, and the number of workgroups that share the keys of a row, joined by a second launch if above 1.
  * n >= 1, pos + n <= 2^30. */
 sa_status sa_cache_attend_plan(const sa_ctx *ctx, int64_t n, int64_t pos, int32_t *rows, int32_t *splits);
+
+/* Tokens pos .. pos + n - 1 of a cache that holds `tokens` (which says what stands in full blocks), as bf16 into K, V
+ * [n_kv_heads][n]: exactly the values that the other readers see, for sa_estimate_patterns, sa_sparse_prefill or another program.
+ * K.data or V.data may be NULL: that side is left out.  K and V must not overlap each other.  n <= 2^25, pos + n <= tokens; n = 0 does nothing. */
+sa_status sa_cache_read(sa_ctx *ctx, const sa_cache *cache, int64_t tokens, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                        void *hip_stream);
+
+/* ---- the cache in 4 bits -----------------------------------------------------------------------------
+ * DEVICE buffers owned by the caller, 136 bytes for a token and KV head (8 bits: 256, bf16: 512).  A row (a token of a KV head) has four
+ * groups of 32 adjacent elements; a group has 32 codes of OCP e2m1 (a sign, and 0 0.5 1 1.5 2 3 4 6) and one scale 2^e, kept as the byte e + 127
+ * (OCP E8M0).  A key is code * 2^e, exactly a bf16 value; a group whose byte is 255 is NaN.  There are no blocks: a token stands by itself, may
+ * be taken back and written again, and what stands behind the tokens is never read.
+ *   k, v              [n_kv_heads][capacity][64]  codes, element 2i of a row in the lower half of byte i
+ *   k_scale, v_scale  [n_kv_heads][capacity][4]   scale bytes
+ * k and v 16-byte, scales 4-byte aligned. */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+  int64_t capacity; /* tokens, 1 .. 2^30 */
+} sa_cache4;
+
+/* Byte sizes of the four buffers, in sa_cache4 member order. */
+sa_status sa_cache4_bytes(const sa_ctx *ctx, int64_t capacity, size_t sizes[4]);
+
+/* K, V [n_kv_heads][n] (rotated where the model rotates) into tokens pos .. pos + n - 1.  A group gets the least e in [-100, 125] with
+ * (largest magnitude) < 7 * 2^e, 0 if all its values are 0, and the codes nearest to value / 2^e (ties to even); magnitudes from 7 * 2^125 on
+ * become 6 * 2^125.  A group with a NaN or an infinity becomes NaN: the type has neither.  n <= 2^25, pos + n <= capacity; n = 0 does
+ * nothing. */
+sa_status sa_cache4_append(sa_ctx *ctx, const sa_cache4 *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *hip_stream);
+
+/* sa_cache_read on this cache: tokens pos .. pos + n - 1 as bf16. */
+sa_status sa_cache4_read(sa_ctx *ctx, const sa_cache4 *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *hip_stream);
+
+/* sa_cache_decode on this cache: same index, same kept keys, same q, o and pos, same use of ctx's workspace. */
+sa_status sa_cache4_decode(sa_ctx *ctx, const sa_cache4 *cache, const void *q, sa_index idx, int64_t pos, void *o, void *hip_stream);
+
+/* sa_cache_attend on this cache: same Q, O, n, pos and scratch (sa_cache_attend_scratch_bytes), same limits and roundings.  Scores take
+ * an element of Q to 2^-13.9 of the largest of its group of 32 or better. */
+sa_status sa_cache4_attend(sa_ctx *ctx, const sa_cache4 *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
+                           void *scratch_dev, size_t scratch_bytes, void *hip_stream);
+/* sa_cache_attend_plan of such a call. */
+sa_status sa_cache4_attend_plan(const sa_ctx *ctx, int64_t n, int64_t pos, int32_t *rows, int32_t *splits);
 
 const char *sa_last_error(const sa_ctx *ctx);
 

@@ -65,6 +65,10 @@ class SaCache(C.Structure):
                 ("k_open", C.c_void_p), ("v_open", C.c_void_p), ("capacity", C.c_int64), ("type", C.c_int32)]
 
 
+class SaCache4(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("capacity", C.c_int64)]
+
+
 _lib = None
 
 
@@ -107,8 +111,16 @@ def library():
         lib.sa_cache_attend_scratch_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]
         lib.sa_cache_attend_plan.argtypes = [vp, C.c_int64, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         lib.sa_cache_attend.argtypes = [vp, C.POINTER(SaCache), SaRows, C.c_int64, C.c_int64, SaRows, vp, C.c_size_t, vp]
+        lib.sa_cache_read.argtypes = [vp, C.POINTER(SaCache), C.c_int64, SaRows, SaRows, C.c_int64, C.c_int64, vp]
+        lib.sa_cache4_bytes.argtypes = [vp, C.c_int64, C.POINTER(C.c_size_t)]
+        lib.sa_cache4_append.argtypes = [vp, C.POINTER(SaCache4), SaRows, SaRows, C.c_int64, C.c_int64, vp]
+        lib.sa_cache4_read.argtypes = [vp, C.POINTER(SaCache4), SaRows, SaRows, C.c_int64, C.c_int64, vp]
+        lib.sa_cache4_decode.argtypes = [vp, C.POINTER(SaCache4), vp, SaIndex, C.c_int64, vp, vp]
+        lib.sa_cache4_attend_plan.argtypes = [vp, C.c_int64, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        lib.sa_cache4_attend.argtypes = [vp, C.POINTER(SaCache4), SaRows, C.c_int64, C.c_int64, SaRows, vp, C.c_size_t, vp]
         for f in ("sa_rotary_create", "sa_rotary_embed", "sa_cache_bytes", "sa_cache_append", "sa_cache_decode",
-                  "sa_cache_attend_scratch_bytes", "sa_cache_attend_plan", "sa_cache_attend"):
+                  "sa_cache_attend_scratch_bytes", "sa_cache_attend_plan", "sa_cache_attend", "sa_cache_read", "sa_cache4_bytes",
+                  "sa_cache4_append", "sa_cache4_read", "sa_cache4_decode", "sa_cache4_attend_plan", "sa_cache4_attend"):
             getattr(lib, f).restype = st
         for f in ("sa_default_budgets", "sa_create", "sa_scores_bytes", "sa_index_bytes",
                   "sa_workspace_bytes", "sa_set_workspace", "sa_estimate_patterns",
@@ -264,7 +276,7 @@ def sa_cache_bytes(ctx, capacity):
 
 
 def _cache(cache):
-    return cache.struct() if isinstance(cache, Cache) else cache
+    return cache.struct() if isinstance(cache, (Cache, Cache4)) else cache
 
 
 def sa_cache_append(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
@@ -290,6 +302,42 @@ def sa_cache_attend_plan(ctx, n, pos):
 
 def sa_cache_attend(ctx, cache, Q: SaRows, n, pos, O: SaRows, scratch, scratch_bytes, stream=None):
     _check(library().sa_cache_attend(ctx, _cache(cache), Q, n, pos, O, _ptr(scratch), scratch_bytes, stream), ctx)
+
+
+def sa_cache_read(ctx, cache, tokens, K: SaRows, V: SaRows, n, pos, stream=None):
+    """K, V as _rows makes them; an empty SaRows() leaves a side out."""
+    _check(library().sa_cache_read(ctx, _cache(cache), tokens, K, V, n, pos, stream), ctx)
+
+
+def sa_cache4_bytes(ctx, capacity):
+    out = (C.c_size_t * 4)()
+    _check(library().sa_cache4_bytes(ctx, capacity, out))
+    return list(out)
+
+
+def sa_cache4_append(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
+    _check(library().sa_cache4_append(ctx, _cache(cache), K, V, n, pos, stream), ctx)
+
+
+def sa_cache4_read(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
+    """K, V as _rows makes them; an empty SaRows() leaves a side out."""
+    _check(library().sa_cache4_read(ctx, _cache(cache), K, V, n, pos, stream), ctx)
+
+
+def sa_cache4_decode(ctx, cache, q, index: SaIndex, pos, o, stream=None):
+    _check(library().sa_cache4_decode(ctx, _cache(cache), _ptr(q), index, pos, _ptr(o), stream), ctx)
+
+
+def sa_cache4_attend_plan(ctx, n, pos):
+    """(query rows of a workgroup, splits of the keys) of sa_cache4_attend at these sizes."""
+    rows, splits = C.c_int32(), C.c_int32()
+    _check(library().sa_cache4_attend_plan(ctx, n, pos, C.byref(rows), C.byref(splits)))
+    return rows.value, splits.value
+
+
+def sa_cache4_attend(ctx, cache, Q: SaRows, n, pos, O: SaRows, scratch, scratch_bytes, stream=None):
+    """scratch as for sa_cache_attend."""
+    _check(library().sa_cache4_attend(ctx, _cache(cache), Q, n, pos, O, _ptr(scratch), scratch_bytes, stream), ctx)
 
 
 class Rotary:
@@ -337,6 +385,26 @@ class Cache:
         self.k, self.v, self.k_scale, self.v_scale, self.k_open, self.v_open = self.tensors
         self.heads, self.capacity, self.block, self.type, self.device = heads, capacity, block, cache_type, k.get_device()
         self._struct = SaCache(*[t.data_ptr() for t in self.tensors], capacity, cache_type)
+
+    def struct(self):
+        return self._struct
+
+
+class Cache4:
+    """The four buffers of a 4-bit key/value cache (see sa_cache4 in include/sa.h): k, v uint8 [n_kv_heads, capacity, 64],
+    k_scale, v_scale uint8 [n_kv_heads, capacity, 4], contiguous."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        if k.ndim != 3 or k.shape[2] != 64:
+            raise SaError(1, "k of a 4-bit cache is [n_kv_heads, capacity, 64]")
+        heads, capacity, _ = k.shape
+        self.tensors = (k, v, k_scale, v_scale)
+        for t, last in zip(self.tensors, (64, 64, 4, 4)):
+            if tuple(t.shape) != (heads, capacity, last) or t.element_size() != 1 or not t.is_contiguous() or t.device != k.device:
+                raise SaError(1, f"a cache buffer is not a contiguous tensor of {(heads, capacity, last)} with 1 byte an element on {k.device}")
+        self.k, self.v, self.k_scale, self.v_scale = self.tensors
+        self.heads, self.capacity, self.block, self.device = heads, capacity, None, k.get_device()
+        self._struct = SaCache4(*[t.data_ptr() for t in self.tensors], capacity)
 
     def struct(self):
         return self._struct
@@ -494,24 +562,56 @@ class Session:
         assert [x.nbytes for x in bufs] == sizes
         return Cache(*bufs, cache_type)
 
+    def cache4(self, capacity):
+        """An empty 4-bit cache for `capacity` tokens, for the same calls as cache()."""
+        sizes = sa_cache4_bytes(self.ctx, capacity)
+        bufs = [self.torch.empty((self.cfg.n_kv_heads, capacity, last), dtype=self.torch.uint8, device=self.ws.device) for last in (64, 64, 4, 4)]
+        assert [x.nbytes for x in bufs] == sizes
+        return Cache4(*bufs)
+
     def _own(self, cache):
-        """The cache's struct, if the cache fits the session."""
-        if cache.heads != self._hkv or cache.block != self._block or cache.device != self._gpu:
+        """The cache's struct, if the cache fits the session; a 4-bit cache has no blocks."""
+        if cache.heads != self._hkv or cache.block not in (self._block, None) or cache.device != self._gpu:
             raise SaError(1, f"the cache has {cache.heads} heads and blocks of {cache.block} on device {cache.device}, "
                              f"the session {self._hkv} and {self._block} on {self._gpu}")
         return cache.struct()
 
     def append(self, cache, K, V, pos):
         """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds.  To take tokens back across a block that a call
-        has filled: copies of cache.k_open and cache.v_open from before it, put back, and append() again from its pos on."""
+        has filled: copies of cache.k_open and cache.v_open from before it, put back, and append() again from its pos on; a 4-bit
+        cache has no blocks, append() from any pos on."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
                 return self.append(cache, K, V, pos)
         n = K.shape[1]
         shape = (self._hkv, n, 128)
-        st = self._lib.sa_cache_append(self.ctx, struct, _rows(K, shape, self._bf16, device, "K"), _rows(V, shape, self._bf16, device, "V"),
+        call = self._lib.sa_cache4_append if cache.block is None else self._lib.sa_cache_append
+        st = call(self.ctx, struct, _rows(K, shape, self._bf16, device, "K"), _rows(V, shape, self._bf16, device, "V"),
                                        n, pos, self._raw_stream(device))
+        if st:
+            _check(st, self.ctx)
+
+    def read(self, cache, K, V, pos=0, tokens=None):
+        """Tokens pos, pos + 1, ... of a cache into K, V [n_kv_heads, n, 128] (either may be None).  tokens: how many the cache holds,
+        pos + n if it is left out (a 4-bit cache is read the same for any)."""
+        device, struct = self._gpu, self._own(cache)
+        if self._get_device() != device:
+            with self.torch.cuda.device(device):
+                return self.read(cache, K, V, pos, tokens)
+        if K is None and V is None:
+            raise SaError(1, "K or V is needed")
+        n = (V if K is None else K).shape[1]
+        shape, bf16 = (self._hkv, n, 128), self._bf16
+        k = _NO_ROWS if K is None else _rows(K, shape, bf16, device, "K")
+        v = _NO_ROWS if V is None else _rows(V, shape, bf16, device, "V")
+        held = pos + n if tokens is None else tokens
+        if held < pos + n:
+            raise SaError(1, f"the cache holds {held} tokens, not {pos + n}")
+        if cache.block is None:
+            st = self._lib.sa_cache4_read(self.ctx, struct, k, v, n, pos, self._raw_stream(device))
+        else:
+            st = self._lib.sa_cache_read(self.ctx, struct, held, k, v, n, pos, self._raw_stream(device))
         if st:
             _check(st, self.ctx)
 
@@ -525,7 +625,8 @@ class Session:
         for t in (q, o):
             if t.shape != shape or t.dtype is not bf16 or not t.is_contiguous() or t.get_device() != device:
                 raise SaError(1, f"q and o must be contiguous bf16 tensors {list(shape)} on the session's device")
-        sa_cache_decode(self.ctx, struct, q, self._index(), pos, o, self._raw_stream(device))
+        step = sa_cache4_decode if cache.block is None else sa_cache_decode
+        step(self.ctx, struct, q, self._index(), pos, o, self._raw_stream(device))
 
     def attend_scratch(self):
         """The session's scratch of attend(), allocated at the first use and kept: attend() calls that may overlap in time,
@@ -548,7 +649,8 @@ class Session:
         n = Q.shape[1]
         shape = (self._hq, n, 128)
         q = _rows(Q, shape, self._bf16, device, "Q")
-        st = self._lib.sa_cache_attend(self.ctx, struct, q, n, pos, q if O is Q else _rows(O, shape, self._bf16, device, "O"), scratch, size,
+        call = self._lib.sa_cache4_attend if cache.block is None else self._lib.sa_cache_attend
+        st = call(self.ctx, struct, q, n, pos, q if O is Q else _rows(O, shape, self._bf16, device, "O"), scratch, size,
                                        self._raw_stream(device))
         if st:
             _check(st, self.ctx)

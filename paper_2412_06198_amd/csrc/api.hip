@@ -31,7 +31,7 @@ void carve(sa_ctx *c) {
   c->off[6] = o; o += 256;
   c->off[7] = o; o += align256(sa::index_scratch_bytes(s));
   c->off[8] = o; o += align256((size_t)s.Hq * (s.N / 32) * 4);
-  c->off[9] = o; o += align256(std::max(sa::decode_partial_bytes(s), sa::cache_decode_partial_bytes(s)));
+  c->off[9] = o; o += align256(std::max({sa::decode_partial_bytes(s), sa::cache_decode_partial_bytes(s), sa::cache4_decode_partial_bytes(s)}));
   c->off[10] = o; o += align256(sa::attn_item_bytes(s));
   c->off[11] = o; o += align256(sa::attn_tile_bytes(s));
   c->ws_bytes = o;
@@ -439,15 +439,20 @@ sa_status sa_cache_append(sa_ctx *c, const sa_cache *cache, sa_rows K, sa_rows V
   return hip_result(c, sa::launch_cache_append(c->sh, *cache, K, V, n, pos, (hipStream_t)stream));
 }
 
-sa_status sa_cache_decode(sa_ctx *c, const sa_cache *cache, const void *q, sa_index idx, int64_t pos, void *o,
-                          void *stream) {
-  if (!c) return SA_ERR_INVALID_ARG;
+static sa_status check_cached_step(sa_ctx *c, const void *q, sa_index idx, int64_t pos, const void *o) {
   if (!q || !o || !idx.n_cols || !idx.cols || !idx.n_offs || !idx.offs || !idx.rowptr || !idx.blkcols)
     return fail(c, SA_ERR_INVALID_ARG, "null pointer");
   if (((uintptr_t)q | (uintptr_t)o) & 15) return fail(c, SA_ERR_INVALID_ARG, "q, o must be 16-byte aligned");
   if (pos < c->sh.N || pos - c->sh.N >= (1 << 20))
     return fail(c, SA_ERR_INVALID_ARG, "pos must lie in [seq_len, seq_len + 2^20)");
-  const sa_status s = check_cache(c, cache, pos + 1);
+  return SA_OK;
+}
+
+sa_status sa_cache_decode(sa_ctx *c, const sa_cache *cache, const void *q, sa_index idx, int64_t pos, void *o,
+                          void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  sa_status s = check_cached_step(c, q, idx, pos, o);
+  if (s == SA_OK) s = check_cache(c, cache, pos + 1);
   if (s != SA_OK) return s;
   if (!c->have_ws) return fail(c, SA_ERR_INVALID_ARG, "no workspace attached");
   return hip_result(c, sa::launch_cache_decode(c->sh, c->ws.dec_part, *cache, (const uint16_t *)q, idx, (int)pos,
@@ -474,22 +479,119 @@ sa_status sa_cache_attend_plan(const sa_ctx *c, int64_t n, int64_t pos, int32_t 
   return SA_OK;
 }
 
-sa_status sa_cache_attend(sa_ctx *c, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
-                          void *scratch, size_t scratch_bytes, void *stream) {
-  if (!c) return SA_ERR_INVALID_ARG;
-  if (!attend_sizes(c, n, pos)) return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
-  const sa_status s = check_cache(c, cache, pos + n);
-  if (s != SA_OK) return s;
+// Scratch and tensors of a call, strides filled in; n = 0 needs no tensors.
+static sa_status check_attend_tensors(sa_ctx *c, sa_rows *Q, int64_t n, sa_rows *O, const void *scratch, size_t scratch_bytes) {
   if (!scratch || ((uintptr_t)scratch & 255)) return fail(c, SA_ERR_INVALID_ARG, "scratch must be a 256-byte aligned device pointer");
   if (scratch_bytes < sa::attend_scratch_bytes(c->sh))
     return fail(c, SA_ERR_BUFFER_TOO_SMALL, "scratch smaller than sa_cache_attend_scratch_bytes");
   if (n == 0) return SA_OK;
-  const char *why = resolve_rows(&Q, c->sh.Hq, n, false);
-  if (!why) why = resolve_rows(&O, c->sh.Hq, n, true);
+  const char *why = resolve_rows(Q, c->sh.Hq, n, false);
+  if (!why) why = resolve_rows(O, c->sh.Hq, n, true);
   if (why) return fail(c, SA_ERR_INVALID_ARG, why);
-  if (Q.data == O.data && (Q.head_stride != O.head_stride || Q.row_stride != O.row_stride))
+  if (Q->data == O->data && (Q->head_stride != O->head_stride || Q->row_stride != O->row_stride))
     return fail(c, SA_ERR_INVALID_ARG, "in place, the strides must be the same");
+  return SA_OK;
+}
+
+sa_status sa_cache_attend(sa_ctx *c, const sa_cache *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
+                          void *scratch, size_t scratch_bytes, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (!attend_sizes(c, n, pos)) return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
+  sa_status s = check_cache(c, cache, pos + n);
+  if (s == SA_OK) s = check_attend_tensors(c, &Q, n, &O, scratch, scratch_bytes);
+  if (s != SA_OK || n == 0) return s;
   return hip_result(c, sa::launch_cache_attend(c->sh, *cache, Q, (int)n, (int)pos, O, scratch, (hipStream_t)stream));
+}
+
+// The sides of a read that are wanted, their strides filled in.
+static const char *resolve_outputs(sa_rows *K, sa_rows *V, int heads, int64_t n) {
+  if (!K->data && !V->data) return "null pointer";
+  const char *why = K->data ? resolve_rows(K, heads, n, true) : nullptr;
+  return why || !V->data ? why : resolve_rows(V, heads, n, true);
+}
+
+sa_status sa_cache_read(sa_ctx *c, const sa_cache *cache, int64_t tokens, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (n < 0 || pos < 0 || n > kMaxTokens || pos > (int64_t)1 << 30 || tokens > (int64_t)1 << 30 || pos + n > tokens)
+    return fail(c, SA_ERR_INVALID_ARG, "n must lie in [0, 2^25], pos in [0, 2^30], and pos + n must not be above tokens");
+  const sa_status s = check_cache(c, cache, tokens);
+  if (s != SA_OK) return s;
+  if (n == 0) return SA_OK;
+  const char *why = resolve_outputs(&K, &V, c->sh.Hkv, n);
+  if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  return hip_result(c, sa::launch_cache_read(c->sh, *cache, tokens, K, V, n, pos, (hipStream_t)stream));
+}
+
+sa_status sa_cache4_bytes(const sa_ctx *c, int64_t capacity, size_t sizes[4]) {
+  if (!c || !sizes || capacity <= 0 || capacity > (int64_t)1 << 30) return SA_ERR_INVALID_ARG;
+  const size_t rows = (size_t)c->sh.Hkv * (size_t)capacity;
+  sizes[0] = sizes[1] = rows * (sa::kHeadDim / 2);
+  sizes[2] = sizes[3] = rows * (sa::kHeadDim / 32);
+  return SA_OK;
+}
+
+static sa_status check_cache4(sa_ctx *c, const sa_cache4 *h, int64_t tokens) {
+  if (!h || !h->k || !h->v || !h->k_scale || !h->v_scale) return fail(c, SA_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)h->k | (uintptr_t)h->v) & 15) return fail(c, SA_ERR_INVALID_ARG, "the cache's k, v must be 16-byte aligned");
+  if (((uintptr_t)h->k_scale | (uintptr_t)h->v_scale) & 3)
+    return fail(c, SA_ERR_INVALID_ARG, "the cache's scales must be 4-byte aligned");
+  if (h->capacity <= 0 || h->capacity > (int64_t)1 << 30) return fail(c, SA_ERR_INVALID_ARG, "the cache's capacity must lie in [1, 2^30]");
+  if (tokens > h->capacity) return fail(c, SA_ERR_BUFFER_TOO_SMALL, "the cache has no room for that many tokens");
+  return SA_OK;
+}
+
+sa_status sa_cache4_append(sa_ctx *c, const sa_cache4 *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (n < 0 || pos < 0 || n > kMaxTokens || pos > (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "n must lie in [0, 2^25], pos in [0, 2^30]");
+  const sa_status s = check_cache4(c, cache, pos + n);
+  if (s != SA_OK) return s;
+  if (n == 0) return SA_OK;
+  const char *why = resolve_rows(&K, c->sh.Hkv, n, false);
+  if (!why) why = resolve_rows(&V, c->sh.Hkv, n, false);
+  if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  return hip_result(c, sa::launch_cache4_append(c->sh, *cache, K, V, n, pos, (hipStream_t)stream));
+}
+
+sa_status sa_cache4_read(sa_ctx *c, const sa_cache4 *cache, sa_rows K, sa_rows V, int64_t n, int64_t pos, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (n < 0 || pos < 0 || n > kMaxTokens || pos > (int64_t)1 << 30)
+    return fail(c, SA_ERR_INVALID_ARG, "n must lie in [0, 2^25], pos in [0, 2^30]");
+  const sa_status s = check_cache4(c, cache, pos + n);
+  if (s != SA_OK) return s;
+  if (n == 0) return SA_OK;
+  const char *why = resolve_outputs(&K, &V, c->sh.Hkv, n);
+  if (why) return fail(c, SA_ERR_INVALID_ARG, why);
+  return hip_result(c, sa::launch_cache4_read(c->sh, *cache, K, V, n, pos, (hipStream_t)stream));
+}
+
+sa_status sa_cache4_decode(sa_ctx *c, const sa_cache4 *cache, const void *q, sa_index idx, int64_t pos, void *o, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  sa_status s = check_cached_step(c, q, idx, pos, o);
+  if (s == SA_OK) s = check_cache4(c, cache, pos + 1);
+  if (s != SA_OK) return s;
+  if (!c->have_ws) return fail(c, SA_ERR_INVALID_ARG, "no workspace attached");
+  return hip_result(c, sa::launch_cache4_decode(c->sh, c->ws.dec_part, *cache, (const uint16_t *)q, idx, (int)pos,
+                                                (uint16_t *)o, (hipStream_t)stream));
+}
+
+sa_status sa_cache4_attend_plan(const sa_ctx *c, int64_t n, int64_t pos, int32_t *rows, int32_t *splits) {
+  if (!c || !rows || !splits || n == 0 || !attend_sizes(c, n, pos) || pos + n > (int64_t)1 << 30) return SA_ERR_INVALID_ARG;
+  int r, s;
+  sa::cache4_attend_plan(c->sh, (int)n, (int)pos, &r, &s);
+  *rows = r;
+  *splits = s;
+  return SA_OK;
+}
+
+sa_status sa_cache4_attend(sa_ctx *c, const sa_cache4 *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
+                           void *scratch, size_t scratch_bytes, void *stream) {
+  if (!c) return SA_ERR_INVALID_ARG;
+  if (!attend_sizes(c, n, pos)) return fail(c, SA_ERR_INVALID_ARG, "n, pos >= 0 and n * n_q_heads < 2^30 are needed");
+  sa_status s = check_cache4(c, cache, pos + n);
+  if (s == SA_OK) s = check_attend_tensors(c, &Q, n, &O, scratch, scratch_bytes);
+  if (s != SA_OK || n == 0) return s;
+  return hip_result(c, sa::launch_cache4_attend(c->sh, *cache, Q, (int)n, (int)pos, O, scratch, (hipStream_t)stream));
 }
 
 const char *sa_last_error(const sa_ctx *c) { return c ? c->err : "null context"; }

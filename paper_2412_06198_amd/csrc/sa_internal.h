@@ -144,6 +144,18 @@ size_t attend_scratch_bytes(const Shape &sh);
 void cache_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits);
 hipError_t launch_cache_attend(const Shape &sh, const sa_cache &c, sa_rows Q, int n, int pos, sa_rows O,
                                void *scratch, hipStream_t st);
+hipError_t launch_cache_read(const Shape &sh, const sa_cache &c, int64_t tokens, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                             hipStream_t st);
+hipError_t launch_cache4_append(const Shape &sh, const sa_cache4 &c, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                                hipStream_t st);
+hipError_t launch_cache4_read(const Shape &sh, const sa_cache4 &c, sa_rows K, sa_rows V, int64_t n, int64_t pos,
+                              hipStream_t st);
+size_t cache4_decode_partial_bytes(const Shape &sh);
+hipError_t launch_cache4_decode(const Shape &sh, float *partials, const sa_cache4 &c, const uint16_t *q, sa_index idx,
+                                int pos, uint16_t *o, hipStream_t st);
+void cache4_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits);
+hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, int n, int pos, sa_rows O,
+                                void *scratch, hipStream_t st);
 hipError_t launch_sparse_prefill(const Shape &sh, const Workspace &ws, const uint16_t *Q,
                                  const uint16_t *K, const uint16_t *V, sa_index idx, uint16_t *O,
                                  unsigned long long *counters, hipStream_t st);
