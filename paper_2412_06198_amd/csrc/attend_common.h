@@ -126,17 +126,15 @@ __device__ inline void put_waves(const AttendOut &p, int kvh, int r0, int sp, fl
   }
 }
 
-// V of a tile stands in LDS in bf16, key r in 256 bytes with the 16-byte chunk c at c ^ ((r & 3) << 2), or WIDE at c ^ ((r & 3) << 2 | (r >> 2 & 3))
-// where a lane stores whole groups of 32 elements.
 #define SA_VTR(tile, db, key0) \
-  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6 | (WIDE && ((key0) & 8) ? 32 : 0))) + (key0) * 256)))
+  __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)(tile) + ((vbase ^ (unsigned)((db) << 6)) + (key0) * 256)))
 
 // A tile's scores (lane = row, accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4 of HF * 32) into a row's running
 // softmax and its outputs.  masked: keys from place lim + 1 (less 4gg) on are not seen.
 // PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each, which adds to an output as much error as
 // its own rounding does (0.0023 of the outputs' scale, rounding alone 0.0017).  2: a leading part and the rest, 2^-15, by twice
 // the products: 0.0017.  launch_cache_attend says which.
-template <int PARTS, bool WIDE = false, int HF>
+template <int PARTS, int HF>
 __device__ inline void absorb_tile(f32x16 (&sacc)[HF], bool masked, int lim, const uint16_t *Vt, unsigned vbase, float c,
                                    float &m_run, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
