@@ -397,7 +397,7 @@ sa_status sa_cache4_read(sa_ctx *ctx, const sa_cache4 *cache, sa_rows K, sa_rows
 sa_status sa_cache4_decode(sa_ctx *ctx, const sa_cache4 *cache, const void *q, sa_index idx, int64_t pos, void *o, void *hip_stream);
 
 /* sa_cache_attend on this cache: same Q, O, n, pos and scratch (sa_cache_attend_scratch_bytes), same limits and roundings.  Scores take
- * an element of Q to 2^-13.9 of the largest of its group of 32 or better. */
+ * an element of Q, times the softmax scale, to 2^-12.8 of the largest of its group of 32 or better. */
 sa_status sa_cache4_attend(sa_ctx *ctx, const sa_cache4 *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
                            void *scratch_dev, size_t scratch_bytes, void *hip_stream);
 /* sa_cache_attend_plan of such a call. */

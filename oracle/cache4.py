@@ -53,16 +53,22 @@ def read(x):
 E2M3 = np.array([(1 + m / 8) * 2.0 ** (e - 1) if e else m / 8 for e in range(4) for m in range(8)])  # OCP e2m3 magnitudes, by code
 
 
-def query_left_out(q):
-    """What three e2m3 codes of the elements of q [..., 128] (scales 2^e, 2^(e - 4), 2^(e - 8) of a group of 32, the least e >= -92 with every
-    magnitude <= 7.5 * 2^e) leave of them."""
-    r = q.reshape(*q.shape[:-1], -1, GROUP).copy()
+def _bf16(x):
+    """fp32 values rounded to bf16, ties to even."""
+    bits = x.astype(np.float32).view(np.uint32)
+    return ((bits + 0x7FFF + ((bits >> 16) & 1)) & 0xFFFF0000).astype(np.uint32).view(np.float32).astype(np.float64)
+
+
+def query_left_out(q, c=1.0):
+    """What three e2m3 codes of the elements of q [..., 128] times c in fp32 (scales 2^e, 2^(e - 4), 2^(e - 8) of a group of 32, the least
+    e >= -118 with every magnitude <= 7.5 * 2^e; a code is the nearest to what is left, rounded to bf16 first) leave of them."""
+    r = (q.astype(np.float32) * np.float32(c)).astype(np.float64).reshape(*q.shape[:-1], -1, GROUP)
     top = np.abs(r).max(-1)
     m, e = np.frexp(top / 7.5)  # top = 7.5 m 2^e, m in [0.5, 1)
-    s = 2.0 ** np.where(top > 0, np.maximum(e - (m == 0.5), -92), -92)[..., None]
+    s = 2.0 ** np.where(top > 0, np.maximum(e - (m == 0.5), -118), -118)[..., None]
     for k in range(3):
         unit = s * 2.0 ** (-4 * k)
-        a = np.minimum(np.abs(r) / unit, 7.5)
+        a = np.minimum(np.abs(_bf16(r)) / unit, 7.5)
         hi = np.clip(np.searchsorted(E2M3, a), 1, 31)
         below, above = a - E2M3[hi - 1], E2M3[hi] - a
         r = r - np.copysign(E2M3[np.where((above < below) | ((above == below) & (hi % 2 == 0)), hi, hi - 1)] * unit, r)

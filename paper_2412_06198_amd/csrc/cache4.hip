@@ -30,11 +30,6 @@ struct Append4Args {
 template <int CTRL>
 __device__ inline uint32_t row_moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
 
-__device__ inline uint32_t max_halves(uint32_t a, uint32_t b) {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-
 // Grid (ceil(n / 64), KV heads, K or V).
 __global__ __launch_bounds__(kThreads) void append4_kernel(Append4Args p) {
   const int side = blockIdx.z, h = blockIdx.y, ln = threadIdx.x & 15;

@@ -2,10 +2,11 @@
 // online softmax, for n from one token to thousands.  The rows, tiles and splits are those of the 8-bit cache (cache_attend.hip); what the 4 bits
 // change is that K goes into the products as it is: its codes and scales are the operands of the scaled matrix instructions, and
 // a group of 32 elements is what a lane holds of one.
-//   Q, in bf16, becomes the sum of three codes of 6 bits (e2m3), scales 2^e, 2^(e - 4), 2^(e - 8) for a group of 32, the least e with
-//   every |q| <= 7.5 2^e: each takes what the ones before leave, all steps exact but the last, which leaves out 2^-12 scales at most, 2^-13.9
-//   of the group's largest.  Codes of 4 and 6 bits multiply at twice the rate of 8 and four times that of 16, so three of them cost
+//   Q, times the softmax scale and log2(e) in fp32, becomes the sum of three codes of 6 bits (e2m3), scales 2^e, 2^(e - 4), 2^(e - 8) for a group of
+//   32, the least e with every magnitude <= 7.5 2^e: each takes what the ones before leave, and what the last leaves is 2^-10.9 scales
+//   at most, 2^-12.8 of the group's largest.  Codes of 4 and 6 bits multiply at twice the rate of 8 and four times that of 16, so three of them cost
 //   three quarters of two codes of 8 bits or of one product in bf16.
+//   The products start at minus the row's reference in place of 0: what comes out is the exponent of a probability.
 //   V has to be multiplied with probabilities, which need bf16: its codes are turned into bf16 on their way into LDS.
 #include <algorithm>
 #include <cmath>
@@ -18,10 +19,10 @@ namespace sa {
 namespace {
 
 typedef int i32x6 __attribute__((ext_vector_type(6)));
-typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 constexpr int kRowsMany = 128, kRowsFew = 32;  // query rows of a workgroup
+constexpr int kCodes = 3;                      // of an element of Q
 
 struct Attend4Args : AttendOut {
   const uint16_t *Q;
@@ -31,53 +32,172 @@ struct Attend4Args : AttendOut {
   int tiles;         // row tiles
   int turn;          // many rows: row tiles from the last one down, this many, then from the first one up
   int pos, tokens;   // of the first query; in the cache
-  float c;           // softmax scale * log2(e)
+  float c;           // softmax scale * log2(e), which goes into Q
 };
 
-// The three codes of 32 elements, and their scales, one a byte.
-__device__ inline uint32_t cut_query(const uint16_t *at, i32x6 (&code)[3]) {
-  uint4 x[4];
-  uint32_t top = 0;
+// The codes of 32 elements times c, and their scales, one a byte.
+template <int CODES>
+__device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[CODES]) {
+  uint32_t w[16], top = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    x[k] = ((const uint4 *)at)[k];
-    const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+  for (int k = 0; k < 4; ++k) *(uint4 *)&w[4 * k] = ((const uint4 *)at)[k];
+  f32x16 even, odd;  // elements 2k, 2k + 1, as the conversion to codes takes them
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+  for (int k = 0; k < 16; ++k) {
+    top = max_halves(top, w[k] & 0x7FFF7FFFu);
+    even[k] = __uint_as_float(w[k] << 16) * c;
+    odd[k] = __uint_as_float(w[k] & 0xFFFF0000u) * c;
   }
-  // 7.5 = 1.875 * 2^2; the scales stay bytes, and what underflows is below 2^-100.  With an infinity or NaN every score is NaN.
-  const int e = max((int)(top >> 7) - 129 + ((top & 0x7Fu) > 0x70u ? 1 : 0), -92);
-  bf16x32 r = __builtin_bit_cast(bf16x32, x);
+  top = max(top & 0xFFFFu, top >> 16);
+  // 7.5 = 1.875 * 2^2; the least of the scales is a normal number.  With an infinity or NaN, or one as a product with c, every score is NaN.
+  const uint32_t bits = __float_as_uint(fabsf(__uint_as_float(top << 16) * c));
+  const int e = max((int)(bits >> 23) - 129 + ((bits & 0x7FFFFFu) > 0x700000u ? 1 : 0), -118);
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < CODES; ++i) {
     const float s = __uint_as_float((uint32_t)(127 + e - 4 * i) << 23);
-    const auto c = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(r, s);
-    code[i] = __builtin_bit_cast(i32x6, c);
-    if (i < 2) {  // what is left, exactly: 8 bits at most
-      const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, s);
+    const auto q = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
+    code[i] = __builtin_bit_cast(i32x6, q);
+    if (i + 1 < CODES) {
+      const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
 #pragma unroll
-      for (int k = 0; k < 32; ++k) r[k] = (__bf16)((float)r[k] - back[k]);
+      for (int k = 0; k < 16; ++k) {
+        even[k] -= back[2 * k];
+        odd[k] -= back[2 * k + 1];
+      }
     }
   }
   const uint32_t b = (uint32_t)(127 + e);
-  return top >= 0x7F80u ? 0x00FFFFFFu : b | (b - 4) << 8 | (b - 8) << 16;
+  return bits < 0x7F800000u ? b | (b - 4) << 8 | (b - 8) << 16 : 0x00FFFFFFu;
 }
 
-template <int A_BYTE, int PART>
-__device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[3], f32x16 acc, uint32_t k_scale, uint32_t q_scale) {
+template <int A_BYTE, int PART, int CODES>
+__device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[CODES], f32x16 acc, uint32_t k_scale, uint32_t q_scale) {
   const i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
   const i32x8 b = {q[PART][0], q[PART][1], q[PART][2], q[PART][3], q[PART][4], q[PART][5], 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 2, A_BYTE, (int)k_scale, PART, (int)q_scale);
 }
 
-// The groups of V of a key that are NaN, for a row that sees it.
-__device__ inline void put_nan(uint32_t bad, bool sees, f32x16 (&o)[4]) {
-  if (bad == 0u) return;
+// A tile's exponents (lane = row, accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4 of HF * 32) into a row's running softmax and its outputs.
+// They are relative to the row's reference m_run, or to 0 before it has one; start: what the next products begin with.
+// masked: keys from place lim + 1 (less 4gg) on are not seen.
+// PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each; 2: a leading part and the rest, 2^-15, by twice
+// the products.  launch_cache4_attend says which.
+template <int PARTS, int HF>
+__device__ inline void absorb_exponents(f32x16 (&sacc)[HF], bool masked, int lim, const uint16_t *Vt, unsigned vbase,
+                                        float &m_run, f32x16 &start, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  if (masked) {
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
-    if ((bad >> db & 1u) != 0u && sees)
+    for (int hf = 0; hf < HF; ++hf)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[db][r] = NAN;
+      for (int r = 0; r < 16; ++r)
+        if (32 * hf + 8 * (r / 4) + r % 4 > lim) sacc[hf][r] = -INFINITY;
+  }
+  float tmax = -INFINITY;
+#pragma unroll
+  for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[hf][r]);
+  // The reference moves only when some row's exponents grew beyond 8: until then probabilities may exceed 1 (by at most
+  // 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
+  if (__any(tmax > (m_run == -INFINITY ? -INFINITY : 8.f))) {
+    tmax = max_pair(tmax);
+    const bool first = m_run == -INFINITY;
+    const float d = first ? (tmax == -INFINITY ? 0.f : tmax) : fmaxf(tmax, 0.f);
+    const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-d);  // nothing, or NaN, to rescale before the first
+    if (!first || tmax != -INFINITY) m_run = first ? d : m_run + d;
+    const float ref = m_run == -INFINITY ? 0.f : -m_run;
+    lacc[0] *= alpha;
+    lacc[1] *= alpha;
+#pragma unroll
+    for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[hf][r] -= d;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = ref;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+  }
+  // probabilities, a pair at a time, beside the products
+  auto soft2 = [&](int g, int j) {
+#pragma unroll
+    for (int e = 2 * j; e < 2 * j + 2; ++e) sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(sacc[g >> 1][8 * (g & 1) + e]);
+  };
+  u32x4 pbuf[2][PARTS];
+  auto cvt2 = [&](int g, int j) {
+    const float a = sacc[g >> 1][8 * (g & 1) + 2 * j], b = sacc[g >> 1][8 * (g & 1) + 2 * j + 1];
+    if constexpr (PARTS == 1) {
+      const bf16x2 pr = {(__bf16)a, (__bf16)b};
+      pbuf[g & 1][0][j] = __builtin_bit_cast(uint32_t, pr);
+    } else {  // the leading part is cut, not rounded
+      const uint32_t wa = __float_as_uint(a), wb = __float_as_uint(b);
+      const bf16x2 rest = {(__bf16)(a - __uint_as_float(wa & 0xFFFF0000u)), (__bf16)(b - __uint_as_float(wb & 0xFFFF0000u))};
+      pbuf[g & 1][0][j] = __builtin_amdgcn_perm(wb, wa, 0x07060302u);
+      pbuf[g & 1][1][j] = __builtin_bit_cast(uint32_t, rest);
+    }
+  };
+  // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
+  // 4x4x4 products with ones do it on the matrix pipe.
+  const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+  s16x4 vlo[4], vhi[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) soft2(0, j);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    vlo[i] = SA_VTR(Vt, i & 3, 0);
+    vhi[i] = SA_VTR(Vt, i & 3, 8);
+  }
+#pragma unroll
+  for (int j = 0; j < 3; ++j) cvt2(0, j);
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int i = 0; i < 8 * HF; ++i) {
+    const int g = i >> 2, db = i & 3;
+    if (db == 0) {
+      cvt2(g, 3);
+#pragma unroll
+      for (int x = 0; x < PARTS; ++x) asm("" : "+v"(pbuf[g & 1][x]));
+    }
+    const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) {
+      const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1][x]);
+      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
+      const s16x8 ps = __builtin_bit_cast(s16x8, pb);
+      if (db == 0)
+        lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+      if (db == 3)
+        lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+    }
+    if (i + 4 < 8 * HF) {
+      vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
+      vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
+    }
+    if (g + 1 < 2 * HF) {
+      soft2(g + 1, db);
+      if (db > 0) cvt2(g + 1, db - 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __builtin_amdgcn_s_setprio(0);
+}
+
+// The groups of V that are NaN among the keys first .. first + 63 (rowbad: a byte for each, a bit for each group; 0 from key `end` on), for a row
+// that sees keys up to `see`.
+__device__ inline void put_nan(const uint8_t *rowbad, int first, int end, int see, f32x16 (&o)[4]) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t mine = first + lane < end ? rowbad[lane] : 0u;
+  for (uint64_t which = __ballot(mine != 0u); which != 0ull; which &= which - 1ull) {
+    const int at = __ffsll((unsigned long long)which) - 1;
+    const uint32_t bad = (uint32_t)__shfl((int)mine, at);
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+      if ((bad >> db & 1u) != 0u && first + at <= see)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = NAN;
+  }
 }
 
 // 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads the half row of K
@@ -128,10 +248,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   if (t < t_end) fetch(t);
 
   // Q: the groups 2gg and 2gg + 1 of a row, as the lane's K
-  i32x6 qc[2][3];
+  i32x6 qc[2][kCodes];
   uint32_t qs[2];
 #pragma unroll
-  for (int s = 0; s < 2; ++s) qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, qc[s]);
+  for (int s = 0; s < 2; ++s) qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, p.c, qc[s]);
 
   f32x16 oacc[4];
 #pragma unroll
@@ -139,6 +259,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
   float m_run = -INFINITY;
+  f32x16 start = {};  // minus the reference, 0 before there is one
   f32x4 lacc[2] = {};
 
   unsigned vbase;
@@ -168,8 +289,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
         *(uint4 *)((char *)lds.v[wave] + r * 256 + (((4 * (lane & 3) + k) ^ ((r & 3) * 5)) << 4)) = decode4_8(w[k], s);
     }
     const uint32_t ksw = ks >> (16 * gg);
-    f32x16 sacc[1] = {};  // S^T = K Q^T
-    sacc[0] = score_product<0, 0>(kc[0], qc[0], sacc[0], ksw, qs[0]);
+    asm("" : "+v"(start));  // kept, not made anew
+    f32x16 sacc[1];  // S^T = K Q^T
+    sacc[0] = score_product<0, 0>(kc[0], qc[0], start, ksw, qs[0]);
     sacc[0] = score_product<0, 1>(kc[0], qc[0], sacc[0], ksw, qs[0]);
     sacc[0] = score_product<0, 2>(kc[0], qc[0], sacc[0], ksw, qs[0]);
     sacc[0] = score_product<1, 0>(kc[1], qc[1], sacc[0], ksw, qs[1]);
@@ -177,25 +299,86 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
     sacc[0] = score_product<1, 2>(kc[1], qc[1], sacc[0], ksw, qs[1]);
     if (t + WK < t_end) fetch(t + WK);
     wave_lds_sync();
-    absorb_tile<PARTS>(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, p.c, m_run, lacc, oacc);
+    absorb_exponents<PARTS>(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, m_run, start, lacc, oacc);
     wave_lds_sync();
   }
   if (t_end > t_masked) {
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) {
       if ((t - t_begin) % WK != wave) continue;  // another wave's tile
-      for (int j = t * KT; j < (t + 1) * KT; ++j) put_nan(rowbad[j - t_masked * KT], j <= see, oacc);
+      put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, see, oacc);
     }
   }
   const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
   put_waves(p, kvh, r0, sp, m_run, l_run, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
-// Many rows: four waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
+// Many rows: WAVES waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
 // in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.
-__global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p) {
-  constexpr int KT = 64;
-  constexpr int kMasked = 3;  // tiles that some rows see and others do not, at most: 127 keys
+constexpr int kTile = 64;
+
+// What a lane has of its row (lane & 31 of the wave's).
+struct RowSet {
+  i32x6 qc[2][kCodes];
+  uint32_t qs[2];
+  float m, l;         // the reference of its exponents, the sum of its probabilities
+  int row, see, all;  // the row; the last key that it sees; the last that every row of the wave sees
+};
+
+// K Q^T of half a tile (the codes of d-slab S) for both halves of the keys, product I of kCodes.
+template <int S, int I>
+__device__ inline void score_pair(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (&e)[2], const uint32_t (&ks)[2]) {
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) e[hf] = score_product<S, I>(kf[S][hf], r.qc[S], S == 0 && I == 0 ? f32x16{} : e[hf], ks[hf], r.qs[S]);
+}
+
+// K Q^T of a tile.
+__device__ inline void scores(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (&e)[2], const uint32_t (&ks)[2]) {
+  score_pair<0, 0>(kf, r, e, ks);
+  score_pair<0, 1>(kf, r, e, ks);
+  if constexpr (kCodes > 2) score_pair<0, kCodes - 1>(kf, r, e, ks);
+  score_pair<1, 0>(kf, r, e, ks);
+  score_pair<1, 1>(kf, r, e, ks);
+  if constexpr (kCodes > 2) score_pair<1, kCodes - 1>(kf, r, e, ks);
+}
+
+template <int N>
+struct Int { static constexpr int value = N; };
+
+// Probabilities of pairs N .. N + COUNT - 1 of 16 (a pair: accumulators 2N, 2N + 1), rounded to bf16, as the products take them.
+template <int N, int COUNT>
+__device__ inline void probabilities(f32x16 (&e)[2], u32x4 (&pb)[4]) {
+#pragma unroll
+  for (int n = N; n < N + COUNT; ++n) {
+    const float a = __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7)]), b = __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7) + 1]);
+    const bf16x2 pr = {(__bf16)a, (__bf16)b};
+    pb[n >> 2][n & 3] = __builtin_bit_cast(uint32_t, pr);
+  }
+}
+
+// Keys that a row does not see, from place lim + 1 (less 4gg) of the tile on.
+__device__ inline void hide(f32x16 (&e)[2], int lim) {
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (32 * hf + 8 * (k / 4) + k % 4 > lim) e[hf][k] = -INFINITY;
+}
+// The largest of a row's exponents of a tile.
+__device__ inline float largest(const f32x16 (&e)[2]) {
+  float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    top[0] = fmaxf(top[0], e[0][k]);
+    top[1] = fmaxf(top[1], e[1][k]);
+  }
+  return max_pair(fmaxf(top[0], top[1]));
+}
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args p) {
+  constexpr int KT = kTile, ROWS = 32 * WAVES;
+  constexpr int kMasked = ROWS / KT + 1;  // tiles that some rows see and others do not, at most: ROWS - 1 keys
+  constexpr int NV = 8 / WAVES;           // 8-code pieces of V of a tile that a thread has, over 4: 4 (WAVES 4) or 2
   __shared__ __attribute__((aligned(16))) uint8_t Ks[2][KT * kRow4];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[2][KT * 128];
   __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles: a bit for each group of V that is NaN
@@ -205,17 +388,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then row tiles
   const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, down = rest / p.S;
   const int rt = down < p.turn ? p.tiles - 1 - down : down - p.turn;
-  const int r0 = rt * kRowsMany, r_last = min(r0 + kRowsMany, p.rows) - 1;
+  const int r0 = rt * ROWS, r_last = min(r0 + ROWS, p.rows) - 1;
   const int seen_all = p.pos + r0 / p.g;                // last key that every row of the workgroup sees
   const int t_masked = (seen_all + 1) / KT;             // first tile that some do not
   const int n_tiles = (p.pos + r_last / p.g) / KT + 1;  // tiles that some row sees
   const int per = (n_tiles + p.S - 1) / p.S;
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
-
-  // this lane's row, and the last keys that it, its wave's first and its wave's last row see
-  const int wr0 = min(r0 + 32 * wave, p.rows - 1), wr1 = min(r0 + 32 * wave + 31, p.rows - 1);
-  const int row = min(r0 + 32 * wave + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g);
-  const int see = p.pos + tok, see0 = p.pos + wr0 / p.g, see1 = p.pos + wr1 / p.g;
 
   const size_t first = (size_t)kvh * p.capacity;
   const uint8_t *__restrict__ Kh = p.K + first * kRow4, *__restrict__ Vh = p.V + first * kRow4;
@@ -223,118 +401,213 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 
   // ---- K: 64 rows of 64 bytes, the 16-byte chunk c of row r in place c ^ (r / 4) % 4, so that b128 reads of 16 rows hit 64 banks (the
   // lane that owns place x of row r reads chunk x ^ (r / 4) % 4).  Behind the tokens the last row again, here and below: nobody sees it there.
-  const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + wave * 1024;
-  const int krow = 16 * wave + (lane >> 2), kch = ((lane & 3) ^ (lane >> 4)) << 4;
+  const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + (wave & 3) * 1024;
+  const int krow = 16 * (wave & 3) + (lane >> 2), kch = ((lane & 3) ^ (lane >> 4)) << 4;
   auto issue_k = [&](int t, int buf) {
+    if (WAVES > 4 && wave >= 4) return;
     const unsigned at = (unsigned)(min(krow, p.tokens - 1 - t * KT) * kRow4 + kch);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(Kh + (size_t)t * KT * kRow4),
                  "s"(ldsK + (unsigned)(buf * KT * kRow4)) : "memory");
   };
-  uint32_t ks[2];  // of the keys q and q + 32
+  uint32_t kn[2], ks[2];  // scales of the keys q and q + 32, as read and as the products take them
   auto fetch_ks = [&](int t) {
     const uint32_t *at = ksh + (size_t)t * KT;
     const int lim = p.tokens - 1 - t * KT;
-    ks[0] = at[min(q, lim)];
-    ks[1] = at[min(q + 32, lim)];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) kn[hf] = *(const uint32_t *)((const char *)at + 4u * (unsigned)min(q + 32 * hf, lim));
   };
-  // ---- V: a thread's group of 32 codes, row vrow
-  uint4 vc;
-  uint32_t vs;
-  const int vrow = tid >> 2, vg = tid & 3;
+  const unsigned kbase = (unsigned)(q * kRow4) | (unsigned)(((2 * gg) ^ (q >> 2 & 3)) << 4);
+  uint4 kf[2][2];  // [d-slab][half of the keys]
+  auto read_k = [&](int buf) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) kf[s][hf] = *(const uint4 *)((const char *)&Ks[0][0] + (buf * KT + 32 * hf) * kRow4 + (kbase ^ (unsigned)(s << 4)));
+  };
+  // ---- V: a thread's group of 32 codes of row vrow, or half of it
+  uint32_t vc[NV * 2], vs;
+  const int vrow = tid / (2 * WAVES / 2), vpart = tid % WAVES, vg = vpart * 4 / WAVES;
   auto fetch_v = [&](int t) {
-    const int r = min(vrow, p.tokens - 1 - t * KT);
-    vc = *(const uint4 *)(Vh + (size_t)t * KT * kRow4 + (unsigned)(r * kRow4 + vg * 16));
-    vs = vsh[(size_t)t * KT + (unsigned)r];
+    const unsigned r = (unsigned)min(vrow, p.tokens - 1 - t * KT);
+    const uint8_t *at = Vh + (size_t)t * KT * kRow4;
+    if constexpr (WAVES == 4) {
+      const uint4 x = *(const uint4 *)(at + r * kRow4 + vpart * 16);
+      vc[0] = x.x; vc[1] = x.y; vc[2] = x.z; vc[3] = x.w;
+    } else {
+      const uint2 x = *(const uint2 *)(at + r * kRow4 + vpart * 8);
+      vc[0] = x.x; vc[1] = x.y;
+    }
+    vs = *(const uint32_t *)((const char *)(vsh + (size_t)t * KT) + 4u * r);
   };
   char *const vput = (char *)&Vs[0][0] + vrow * 256;
-  const unsigned vswz = (unsigned)(4 * vg ^ (vrow & 3) * 5) << 4;
+  const unsigned vswz = (unsigned)(16 / WAVES * vpart ^ (vrow & 3) * 5) << 4;
+  auto put_v = [&](int buf, int k, float scale) {
+    *(uint4 *)(vput + buf * KT * 256 + (vswz ^ (unsigned)(k << 4))) = decode4_8(vc[k], scale);
+  };
   // A row that does not see a key gives it weight 0, and 0 x NaN is not 0: in tiles that only some rows see, groups of V
   // that are NaN stay out of the products and come back at the end for the rows that do see them.
   auto screen = [&](int t) {
     const bool bad = (vs >> (8 * vg) & 0xFFu) == kNanScale;
     const uint64_t who = __ballot(bad);
-    if (vg == 0) rowbad[(t - t_masked) * KT + vrow] = (uint8_t)(who >> lane & 15ull);
-    if (bad) { vc = make_uint4(0u, 0u, 0u, 0u); vs = 0x7F7F7F7Fu; }
+    if (vpart == 0) {
+      uint32_t b = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) b |= (uint32_t)(who >> (lane + k * WAVES / 4) & 1ull) << k;
+      rowbad[(t - t_masked) * KT + vrow] = (uint8_t)b;
+    }
+    if (bad) {
+#pragma unroll
+      for (int k = 0; k < NV * 2; ++k) vc[k] = 0u;
+      vs = 0x7F7F7F7Fu;
+    }
   };
-  if (t_begin < t_end) {
-    fetch_v(t_begin);
-    issue_k(t_begin, 0);
-    fetch_ks(t_begin);
-  }
-
-  i32x6 qc[2][3];
-  uint32_t qs[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, qc[s]);
-
-  f32x16 oacc[4];
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-  float m_run = -INFINITY;
-  f32x4 lacc[2] = {};
   unsigned vbase;
   {
     const int r = lane & 15, part = (lane >> 4) & 1, vr = 4 * gg + (r >> 2);
     vbase = (unsigned)(vr * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vr & 3) * 5)) << 4) | (unsigned)((r & 1) << 3);
   }
-  const unsigned kbase = (unsigned)(q * kRow4) | (unsigned)(((2 * gg) ^ (q >> 2 & 3)) << 4);
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-  if (t_begin < t_end) {
-    if (t_begin >= t_masked) screen(t_begin);
-    const float s = scale4(vs >> (8 * vg) & 0xFFu);
-    const uint32_t w[4] = {vc.x, vc.y, vc.z, vc.w};
+  auto begin = [&] {
+    issue_k(t_begin, 0);
+    fetch_v(t_begin);
+    fetch_ks(t_begin);
+  };
+  if (t_begin < t_end) begin();
+  RowSet r;
+  int head, tok;
+  {
+    const int lo = min(r0 + 32 * wave, p.rows - 1);
+    r.row = min(lo + q, p.rows - 1);
+    tok = r.row / p.g;
+    head = kvh * p.g + (r.row - tok * p.g);
+    r.see = p.pos + tok;
+    r.all = p.pos + lo / p.g;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) *(uint4 *)(vput + (vswz ^ (unsigned)(k << 4))) = decode4_8(w[k], s);
-    if (t_begin + 1 < t_end) fetch_v(t_begin + 1);
+    for (int s = 0; s < 2; ++s) r.qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, p.c, r.qc[s]);
   }
-  for (int t = t_begin; t < t_end; ++t) {
-    const int cur = (t - t_begin) & 1, j0 = t * KT;
-    // K of this tile has landed, and V of the next one; after the barrier both buffers of the tile hold it and
-    // every wave is done with the tile before
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    __syncthreads();
-    const uint32_t ksw[2] = {ks[0] >> (16 * gg), ks[1] >> (16 * gg)};
-    if (t + 1 < t_end) {
-      issue_k(t + 1, cur ^ 1);
-      fetch_ks(t + 1);
-      if (t + 1 >= t_masked) screen(t + 1);
-    }
-    // S^T = K Q^T, three products per fragment of K; beside them V of the next tile becomes bf16 (what is left in the
-    // registers, behind the last tile: nobody reads it)
-    const char *Kt = (const char *)&Ks[cur][0];
-    uint4 kf[2][2];
+  f32x16 oacc[4];
+  f32x4 lacc[2];
+  // Probabilities are 2^e as it is: fp32 and bf16 hold them from 2^-126 to 2^127, so that nothing has to be searched, subtracted or rescaled.  Where
+  // that was too little (a row's sum beyond 2^100 or below 2^-80, an output that is no number) the workgroup looks for the rows' largest exponents
+  // and starts anew, with them subtracted.
+  r.m = 0.f;
+  auto run = [&](auto AGAIN) {
+    constexpr bool kAgain = decltype(AGAIN)::value != 0;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int db = 0; db < 4; ++db) oacc[db] = f32x16{};
+    lacc[0] = lacc[1] = f32x4{};
+    if (t_begin < t_end) {
+      if (t_begin >= t_masked) screen(t_begin);
+      {
+        const float s = scale4(vs >> (8 * vg) & 0xFFu);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) kf[s][hf] = *(const uint4 *)(Kt + (kbase ^ (unsigned)(s << 4)) + hf * 32 * kRow4);
-    f32x16 sacc[2] = {};
-    const float vscale = scale4(vs >> (8 * vg) & 0xFFu);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sacc[0] = i == 0 ? score_product<0, 0>(kf[0][0], qc[0], sacc[0], ksw[0], qs[0]) : i == 1 ? score_product<0, 2>(kf[0][0], qc[0], sacc[0], ksw[0], qs[0])
-              : i == 2 ? score_product<1, 0>(kf[1][0], qc[1], sacc[0], ksw[0], qs[1]) : score_product<1, 2>(kf[1][0], qc[1], sacc[0], ksw[0], qs[1]);
-      sacc[1] = i == 0 ? score_product<0, 0>(kf[0][1], qc[0], sacc[1], ksw[1], qs[0]) : i == 1 ? score_product<0, 2>(kf[0][1], qc[0], sacc[1], ksw[1], qs[0])
-              : i == 2 ? score_product<1, 0>(kf[1][1], qc[1], sacc[1], ksw[1], qs[1]) : score_product<1, 2>(kf[1][1], qc[1], sacc[1], ksw[1], qs[1]);
-      if ((i & 1) == 0) {
-        sacc[0] = i == 0 ? score_product<0, 1>(kf[0][0], qc[0], sacc[0], ksw[0], qs[0]) : score_product<1, 1>(kf[1][0], qc[1], sacc[0], ksw[0], qs[1]);
-        sacc[1] = i == 0 ? score_product<0, 1>(kf[0][1], qc[0], sacc[1], ksw[1], qs[0]) : score_product<1, 1>(kf[1][1], qc[1], sacc[1], ksw[1], qs[1]);
+        for (int k = 0; k < NV * 2; ++k) put_v(0, k, s);
       }
-      const uint32_t w = i == 0 ? vc.x : i == 1 ? vc.y : i == 2 ? vc.z : vc.w;
-      *(uint4 *)(vput + (cur ^ 1) * KT * 256 + (vswz ^ (unsigned)(i << 4))) = decode4_8(w, vscale);
-      __builtin_amdgcn_sched_barrier(0);
+      fetch_v(min(t_begin + 1, t_end - 1));
+      for (int t = t_begin; t < t_end; ++t) {
+        const int cur = (t - t_begin) & 1, j0 = t * KT, next = min(t + 1, t_end - 1);
+        // K of this tile has landed, and V of the next one; after the barrier both buffers of the tile hold it and
+        // every wave is done with the tile before
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+        __syncthreads();
+        read_k(cur);
+        ks[0] = kn[0] >> (16 * gg);
+        ks[1] = kn[1] >> (16 * gg);
+        issue_k(next, cur ^ 1);
+        fetch_ks(next);
+        if (t + 1 >= t_masked && t + 1 < t_end) screen(t + 1);
+        const float scale = scale4(vs >> (8 * vg) & 0xFFu);
+        // S^T = K Q^T; beside it V of the next tile becomes bf16 (behind the last tile what is left in the registers: nobody reads it)
+        f32x16 e[2];
+        __builtin_amdgcn_sched_barrier(0);
+#define SA_STEP(S, I, K) \
+        score_pair<S, I>(kf, r, e, ks); \
+        if constexpr ((K) < NV * 2) put_v(cur ^ 1, K, scale); \
+        asm volatile("" : "+v"(e[0]), "+v"(e[1])); \
+        __builtin_amdgcn_sched_barrier(0);
+        SA_STEP(0, 0, 0) SA_STEP(0, 1, 1)
+        if constexpr (kCodes > 2) { SA_STEP(0, kCodes - 1, 2) }
+        SA_STEP(1, 0, 3 - (kCodes < 3)) 
+        if constexpr (kCodes < 3) { SA_STEP(1, 1, 3) } else { SA_STEP(1, 1, 9) SA_STEP(1, kCodes - 1, 9) }
+#undef SA_STEP
+        fetch_v(min(t + 2, t_end - 1));
+        if (kAgain) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            e[0][k] -= r.m;
+            e[1][k] -= r.m;
+          }
+        }
+        if (j0 + KT - 1 > r.all) hide(e, r.see - j0 - 4 * gg);
+        u32x4 pb[4];
+        s16x4 vlo[4], vhi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vlo[i] = SA_VTR(Vs[cur], i & 3, 0);
+          vhi[i] = SA_VTR(Vs[cur], i & 3, 8);
+        }
+        probabilities<0, 4>(e, pb);
+        __builtin_amdgcn_s_setprio(1);
+        // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
+        // 4x4x4 products with ones do it on the matrix pipe.
+        const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+        auto step = [&](auto I) {
+          constexpr int i = decltype(I)::value, g = i >> 2, db = i & 3;
+          const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vlo[db], vhi[db], 0, 1, 2, 3, 4, 5, 6, 7));
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g]), oacc[db], 0, 0, 0);
+          const s16x8 ps = __builtin_bit_cast(s16x8, pb[g]);
+          if constexpr (db == 0) lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+          if constexpr (db == 3) lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+          if constexpr (i + 4 < 16) {
+            vlo[db] = SA_VTR(Vs[cur], db, 16 * ((i + 4) >> 2));
+            vhi[db] = SA_VTR(Vs[cur], db, 16 * ((i + 4) >> 2) + 8);
+          }
+          if constexpr (i < 12) probabilities<i + 4, 1>(e, pb);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        step(Int<0>()); step(Int<1>()); step(Int<2>()); step(Int<3>()); step(Int<4>()); step(Int<5>()); step(Int<6>()); step(Int<7>());
+        step(Int<8>()); step(Int<9>()); step(Int<10>()); step(Int<11>()); step(Int<12>()); step(Int<13>()); step(Int<14>()); step(Int<15>());
+        __builtin_amdgcn_s_setprio(0);
+      }
     }
-    if (t + 2 < t_end) fetch_v(t + 2);
-    if (j0 <= see1) absorb_tile<1>(sacc, j0 + KT - 1 > see0, see - j0 - 4 * gg, Vs[cur], vbase, p.c, m_run, lacc, oacc);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): K of a tile behind the last has landed, before its LDS is another's
+    r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
+  };
+  run(Int<0>());
+  float odd[4] = {};  // 0, or NaN where an output is no number
+#pragma unroll
+  for (int k = 0; k < 16; ++k)
+#pragma unroll
+    for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
+  const bool good = r.see < t_begin * KT || (r.l > 0x1p-80f && r.l < 0x1p100f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f);
+  if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!good)) && t_begin < t_end) {
+    float top = -INFINITY;
+    for (int t = t_begin; t < t_end; ++t) {
+      __syncthreads();
+      issue_k(t, 0);
+      fetch_ks(t);
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+      __syncthreads();
+      ks[0] = kn[0] >> (16 * gg);
+      ks[1] = kn[1] >> (16 * gg);
+      read_k(0);
+      f32x16 e[2];
+      scores(kf, r, e, ks);
+      hide(e, r.see - t * KT - 4 * gg);
+      top = fmaxf(top, largest(e));
+    }
+    __syncthreads();
+    r.m = top == -INFINITY ? 0.f : top;
+    begin();
+    run(Int<1>());
+    if (top == -INFINITY) r.m = top;
   }
   if (t_end > t_masked) {
     __syncthreads();
-    for (int j = max(t_begin, t_masked) * KT; j < t_end * KT; ++j) put_nan(rowbad[j - t_masked * KT], j <= see, oacc);
+    for (int t = max(t_begin, t_masked); t < t_end; ++t) put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
   }
-  const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
-  if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, row, head, tok, sp, gg, m_run, l_run, oacc);
+  if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.see < t_begin * KT ? -INFINITY : r.m, r.l, oacc);
 }
 
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit, as for the 8-bit cache.
@@ -382,7 +655,7 @@ hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, 
   const unsigned grid = (unsigned)(wgs * a.S);
   if (plan.few && a.rows <= 2 * kRowsFew) attend4_few_kernel<2><<<grid, kThreads, 0, st>>>(a);
   else if (plan.few) attend4_few_kernel<1><<<grid, kThreads, 0, st>>>(a);
-  else attend4_rows_kernel<<<grid, kThreads, 0, st>>>(a);
+  else attend4_rows_kernel<4><<<grid, 256, 0, st>>>(a);
   launch_join(a, all, st);
   return hipGetLastError();
 }

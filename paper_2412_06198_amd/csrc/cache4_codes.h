@@ -20,6 +20,11 @@ __device__ inline int scale_exponent4(uint32_t m) {
   return m == 0u ? 0 : min(max(e, -100), 125);
 }
 
+__device__ inline uint32_t max_halves(uint32_t a, uint32_t b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // Pair SLOT of a word of codes, from two bf16 values over `scale`, ties to even.
 template <int SLOT>
 __device__ inline uint32_t encode4_2(uint32_t old, uint32_t pair, float scale) {

@@ -1,7 +1,7 @@
 """Causal attention of the newest tokens over the 4-bit cache, against fp64 on the values that the cache stands for.
 
 Tolerance: half a step of bf16 of the output, 2^-8 |o|; a probability as multiplied, 2^-8 of itself in bf16 or 2^-15 in two parts, normalised
-by the sum of what is multiplied, and fp32 scores as in the decode step, 2^-12: of sum p |v| + |o|; a score off by x, x of
+by the sum of what is multiplied, and fp32 scores as in the decode step, 2^-12: of sum p |v| + |o|; an exponent (of 2) off by x, x ln 2 of
 that too: what the three codes of a query leave out, as the oracle cuts it, times the key."""
 import numpy as np
 import pytest
@@ -37,7 +37,7 @@ def _reference(q, keys, vals, pos, rows, scale=128.0 ** -0.5):
     for h in range(hq):
         s = q[h] @ keys[h // g].T * scale
         s[later] = -np.inf
-        off = np.abs(oc.query_left_out(q[h]) @ keys[h // g].T * scale)
+        off = np.log(2) * np.abs(oc.query_left_out(q[h], np.float32(scale) * np.float32(1.4426950408889634)) @ keys[h // g].T)
         off[later] = 0
         p = np.exp(s - s.max(-1, keepdims=True))
         p /= p.sum(-1, keepdims=True)
