@@ -21,7 +21,7 @@ namespace {
 typedef int i32x6 __attribute__((ext_vector_type(6)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
-constexpr int kRowsMany = 128, kRowsFew = 32;  // query rows of a workgroup
+constexpr int kRowsMany = 128, kRowsFew = 32, kRowsStep = 16;  // query rows of a workgroup
 constexpr int kCodes = 3;                      // of an element of Q
 
 struct Attend4Args : AttendOut {
@@ -36,8 +36,7 @@ struct Attend4Args : AttendOut {
 };
 
 // The codes of 32 elements times c, and their scales, one a byte.
-template <int CODES>
-__device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[CODES]) {
+__device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[kCodes]) {
   uint32_t w[16], top = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) *(uint4 *)&w[4 * k] = ((const uint4 *)at)[k];
@@ -53,11 +52,11 @@ __device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[
   const uint32_t bits = __float_as_uint(fabsf(__uint_as_float(top << 16) * c));
   const int e = max((int)(bits >> 23) - 129 + ((bits & 0x7FFFFFu) > 0x700000u ? 1 : 0), -118);
 #pragma unroll
-  for (int i = 0; i < CODES; ++i) {
+  for (int i = 0; i < kCodes; ++i) {
     const float s = __uint_as_float((uint32_t)(127 + e - 4 * i) << 23);
     const auto q = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
     code[i] = __builtin_bit_cast(i32x6, q);
-    if (i + 1 < CODES) {
+    if (i + 1 < kCodes) {
       const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
@@ -70,8 +69,8 @@ __device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[
   return bits < 0x7F800000u ? b | (b - 4) << 8 | (b - 8) << 16 : 0x00FFFFFFu;
 }
 
-template <int A_BYTE, int PART, int CODES>
-__device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[CODES], f32x16 acc, uint32_t k_scale, uint32_t q_scale) {
+template <int A_BYTE, int PART>
+__device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[kCodes], f32x16 acc, uint32_t k_scale, uint32_t q_scale) {
   const i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
   const i32x8 b = {q[PART][0], q[PART][1], q[PART][2], q[PART][3], q[PART][4], q[PART][5], 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 2, A_BYTE, (int)k_scale, PART, (int)q_scale);
@@ -200,6 +199,18 @@ __device__ inline void put_nan(const uint8_t *rowbad, int first, int end, int se
   }
 }
 
+// Over the four lanes of a row, on each of them.
+__device__ inline float over_blocks(float x) {
+  x = max_pair(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_blocks(float x) {
+  x = sum_pair(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads the half row of K
 // that it multiplies itself.
 template <int PARTS>
@@ -313,10 +324,202 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   put_waves(p, kvh, r0, sp, m_run, l_run, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
-// Many rows: WAVES waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
-// in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.
-constexpr int kTile = 64;
+// Steps: 16 query rows a workgroup, every wave its own keys, tiles of 32 of them.  One v_mfma_scale_f32_16x16x128 takes 16 keys, whole rows of K: a
+// lane reads one group of a key and multiplies it with the same group of its query row (lane & 15).  Half the products, exponentials and registers of 32
+// rows, so that four waves a SIMD, instead of two, have reads on their way.
+__global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p) {
+  constexpr int KT = 32, WK = kThreads / 64, ROWS = kRowsStep;
+  constexpr int kMasked = 2;  // tiles that some rows see and others do not, at most: 15 keys
+  __shared__ __attribute__((aligned(16))) union {
+    uint16_t v[WK][KT * 128];
+    float o[WK][ROWS][kHeadDim];
+  } lds;
+  __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles: a bit for each group of V that is NaN
+  __shared__ float s_m[WK][ROWS], s_l[WK][ROWS];
 
+  const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, b = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // KV heads side by side, then splits, then row tiles from the longest down
+  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = (p.tiles - 1 - rest / p.S) * ROWS;
+  const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
+  const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
+  const int n_tiles = (p.pos + (min(r0 + ROWS, p.rows) - 1) / p.g) / KT + 1;
+  const int per = (n_tiles + p.S - 1) / p.S;
+  const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
+
+  // this lane's row, and the last key that it sees
+  const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
+
+  const size_t first = (size_t)kvh * p.capacity;
+  const uint8_t *__restrict__ Kh = p.K + first * kRow4 + 16 * b, *__restrict__ Vh = p.V + first * kRow4 + 16 * (lane & 3);
+  const uint32_t *__restrict__ ksh = p.k_scale + first, *__restrict__ vsh = p.v_scale + first;
+
+  uint4 kc[2], vc[2];  // a group of the keys q and q + 16; pieces of V: rows lane / 4 and 16 further, a group each
+  uint32_t ks[2], vs[2];
+  auto fetch = [&](int t) {  // behind the tokens the last one again: nobody sees it there
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t kr = min(t * KT + q + 16 * i, p.tokens - 1), vr = min(t * KT + (lane >> 2) + 16 * i, p.tokens - 1);
+      kc[i] = *(const uint4 *)(Kh + kr * kRow4);
+      vc[i] = *(const uint4 *)(Vh + vr * kRow4);
+      ks[i] = ksh[kr];
+      vs[i] = vsh[vr];
+    }
+  };
+  int t = t_begin + wave;
+  if (t < t_end) fetch(t);
+
+  i32x6 qc[kCodes];
+  const uint32_t qs = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 32 * b, p.c, qc);
+
+  f32x4 oacc[8] = {};  // lane = row, accumulator r of piece db <-> element 16db + 4b + r
+  float m_run = -INFINITY, l_run = 0.f;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  // V of a tile in LDS: key r in 256 bytes, the 16-byte chunk c at c ^ place(r), so that the stores of 16 lanes (four keys, a group of each) and the
+  // transposing reads of 64 (16 keys, 16 elements of each) spread over all banks.
+  auto place = [](int r) { return (r & 3) * 5 ^ (r >> 2 & 1) << 1; };
+  unsigned vbase;
+  {
+    const int r = lane & 15, vrow = 4 * b + (r >> 2);
+    vbase = (unsigned)(vrow * 256) | (unsigned)(((r & 3) >> 1 ^ place(vrow)) << 4) | (unsigned)((r & 1) << 3);
+  }
+  for (; t < t_end; t += WK) {
+    // A row that does not see a key gives it weight 0, and 0 x NaN is not 0: in tiles that only some rows see, groups of V
+    // that are NaN stay out of the products and come back at the end for the rows that do see them.
+    if (t >= t_masked) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool bad = (vs[i] >> (8 * (lane & 3)) & 0xFFu) == kNanScale;
+        const uint64_t who = __ballot(bad);
+        if ((lane & 3) == 0) rowbad[(t - t_masked) * KT + (lane >> 2) + 16 * i] = (uint8_t)(who >> lane & 15ull);
+        if (bad) { vc[i] = make_uint4(0u, 0u, 0u, 0u); vs[i] = 0x7F7F7F7Fu; }
+      }
+    }
+    f32x4 e[2];  // exponents: lane = row, accumulator r of half i <-> key 16i + 4b + r
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const i32x8 a = {(int)kc[i].x, (int)kc[i].y, (int)kc[i].z, (int)kc[i].w, 0, 0, 0, 0};
+      const int scale = (int)(ks[i] >> (8 * b));
+      const f32x4 zero = {};
+      auto codes = [&](int k) { return i32x8{qc[k][0], qc[k][1], qc[k][2], qc[k][3], qc[k][4], qc[k][5], 0, 0}; };
+      e[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, codes(0), zero, 4, 2, 0, scale, 0, (int)qs);
+      e[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, codes(1), e[i], 4, 2, 0, scale, 1, (int)qs);
+      e[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, codes(2), e[i], 4, 2, 0, scale, 2, (int)qs);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float s = scale4(vs[i] >> (8 * (lane & 3)) & 0xFFu);
+      const uint32_t w[4] = {vc[i].x, vc[i].y, vc[i].z, vc[i].w};
+      const int r = (lane >> 2) + 16 * i;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *(uint4 *)((char *)lds.v[wave] + r * 256 + (((4 * (lane & 3) + k) ^ place(r)) << 4)) = decode4_8(w[k], s);
+    }
+    const int now = t;
+    if (t + WK < t_end) fetch(t + WK);
+    wave_lds_sync();
+    if ((now + 1) * KT - 1 > seen_all) {
+      const int lim = see - now * KT - 4 * b;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (16 * i + r > lim) e[i][r] = -INFINITY;
+    }
+    float top = fmaxf(fmaxf(fmaxf(e[0][0], e[0][1]), fmaxf(e[0][2], e[0][3])), fmaxf(fmaxf(e[1][0], e[1][1]), fmaxf(e[1][2], e[1][3])));
+    // The reference moves only when some row's exponents grew beyond it by more than 8, see absorb_exponents
+    if (__any(top - m_run > 8.f)) {
+      top = fmaxf(m_run, over_blocks(top));
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (top == -INFINITY ? 0.f : top));
+      m_run = top;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) oacc[db] *= alpha;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    u32x4 lead, rest;  // the probabilities in two parts: cut, and what that leaves
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const float x = __builtin_amdgcn_exp2f(e[i][r] - ref), y = __builtin_amdgcn_exp2f(e[i][r + 1] - ref);
+        l_run += x;
+        l_run += y;
+        const uint32_t wx = __float_as_uint(x), wy = __float_as_uint(y);
+        const bf16x2 left = {(__bf16)(x - __uint_as_float(wx & 0xFFFF0000u)), (__bf16)(y - __uint_as_float(wy & 0xFFFF0000u))};
+        lead[2 * i + r / 2] = __builtin_amdgcn_perm(wy, wx, 0x07060302u);
+        rest[2 * i + r / 2] = __builtin_bit_cast(uint32_t, left);
+      }
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+      const unsigned at = vbase ^ (unsigned)(db << 5);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)lds.v[wave] + at));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((const char *)lds.v[wave] + at + 16 * 256));
+      const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, lead), oacc[db], 0, 0, 0);
+      oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, rest), oacc[db], 0, 0, 0);
+    }
+    wave_lds_sync();
+  }
+  if (t_end > t_masked) {
+    __syncthreads();
+    for (int t = max(t_begin, t_masked); t < t_end; ++t) {
+      if ((t - t_begin) % WK != wave) continue;  // another wave's tile
+      const uint32_t mine = lane < KT ? rowbad[(t - t_masked) * KT + lane] : 0u;
+      for (uint64_t which = __ballot(mine != 0u); which != 0ull; which &= which - 1ull) {
+        const int at = __ffsll((unsigned long long)which) - 1;
+        const uint32_t bad = (uint32_t)__shfl((int)mine, at);
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+          if ((bad >> (db / 2) & 1u) != 0u && t * KT + at <= see) oacc[db] = f32x4{NAN, NAN, NAN, NAN};
+      }
+    }
+  }
+  const float l_row = sum_blocks(l_run);  // the keys of the four lanes of a row
+
+  // ---- the four waves' sums of the same rows, through the LDS of the tiles: O / l in bf16, or the split's sums
+  __syncthreads();
+  if (b == 0) { s_m[wave][q] = m_run; s_l[wave][q] = l_row; }
+#pragma unroll
+  for (int db = 0; db < 8; ++db)
+    *(f32x4 *)&lds.o[wave][q][(16 * db + 4 * b) ^ (q & 7) << 2] = oacc[db];
+  __syncthreads();
+  const int mr = tid >> 4, d0 = (tid & 15) * 8;  // 8 outputs of a row each
+  const int orow = r0 + mr;
+  if (orow >= p.rows) return;
+  float M = -INFINITY, L = 0.f, w[WK];
+#pragma unroll
+  for (int k = 0; k < WK; ++k) M = fmaxf(M, s_m[k][mr]);
+#pragma unroll
+  for (int k = 0; k < WK; ++k) {
+    w[k] = s_m[k][mr] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[k][mr] - M);
+    L += s_l[k][mr] * w[k];
+  }
+  const size_t slot = ((size_t)kvh * p.rows + orow) * p.S + sp;
+  const int otok = orow / p.g;
+  uint16_t *o = p.O + (size_t)(kvh * p.g + orow - otok * p.g) * p.o_hs + (size_t)otok * p.o_rs;
+  if (p.S > 1 && d0 == 0) p.ml[slot] = make_float2(M, L);
+  const float inv = p.S > 1 ? 1.f : 1.f / L;
+  f32x4 x[2] = {};
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int k = 0; k < WK; ++k) x[i] += *(const f32x4 *)&lds.o[k][mr][(d0 + 4 * i) ^ (mr & 7) << 2] * w[k];
+  if (p.S > 1) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(f32x4 *)(p.part + slot * kHeadDim + d0 + 4 * i) = x[i];
+  } else {
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf16x2 u = {(__bf16)(x[i / 2][2 * (i & 1)] * inv), (__bf16)(x[i / 2][2 * (i & 1) + 1] * inv)};
+      y[i] = __builtin_bit_cast(uint32_t, u);
+    }
+    *(uint4 *)(o + d0) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
+}
+
+// Many rows: four waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
+// in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.
 // What a lane has of its row (lane & 31 of the wave's).
 struct RowSet {
   i32x6 qc[2][kCodes];
@@ -336,10 +539,10 @@ __device__ inline void score_pair(const uint4 (&kf)[2][2], const RowSet &r, f32x
 __device__ inline void scores(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (&e)[2], const uint32_t (&ks)[2]) {
   score_pair<0, 0>(kf, r, e, ks);
   score_pair<0, 1>(kf, r, e, ks);
-  if constexpr (kCodes > 2) score_pair<0, kCodes - 1>(kf, r, e, ks);
+  score_pair<0, 2>(kf, r, e, ks);
   score_pair<1, 0>(kf, r, e, ks);
   score_pair<1, 1>(kf, r, e, ks);
-  if constexpr (kCodes > 2) score_pair<1, kCodes - 1>(kf, r, e, ks);
+  score_pair<1, 2>(kf, r, e, ks);
 }
 
 template <int N>
@@ -374,11 +577,9 @@ __device__ inline float largest(const f32x16 (&e)[2]) {
   }
   return max_pair(fmaxf(top[0], top[1]));
 }
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args p) {
-  constexpr int KT = kTile, ROWS = 32 * WAVES;
-  constexpr int kMasked = ROWS / KT + 1;  // tiles that some rows see and others do not, at most: ROWS - 1 keys
-  constexpr int NV = 8 / WAVES;           // 8-code pieces of V of a tile that a thread has, over 4: 4 (WAVES 4) or 2
+__global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p) {
+  constexpr int KT = 64, ROWS = kRowsMany;
+  constexpr int kMasked = 3;  // tiles that some rows see and others do not, at most: 127 keys
   __shared__ __attribute__((aligned(16))) uint8_t Ks[2][KT * kRow4];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[2][KT * 128];
   __shared__ uint8_t rowbad[kMasked * KT];  // keys of the masked tiles: a bit for each group of V that is NaN
@@ -401,10 +602,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args
 
   // ---- K: 64 rows of 64 bytes, the 16-byte chunk c of row r in place c ^ (r / 4) % 4, so that b128 reads of 16 rows hit 64 banks (the
   // lane that owns place x of row r reads chunk x ^ (r / 4) % 4).  Behind the tokens the last row again, here and below: nobody sees it there.
-  const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + (wave & 3) * 1024;
-  const int krow = 16 * (wave & 3) + (lane >> 2), kch = ((lane & 3) ^ (lane >> 4)) << 4;
+  const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + wave * 1024;
+  const int krow = 16 * wave + (lane >> 2), kch = ((lane & 3) ^ (lane >> 4)) << 4;
   auto issue_k = [&](int t, int buf) {
-    if (WAVES > 4 && wave >= 4) return;
     const unsigned at = (unsigned)(min(krow, p.tokens - 1 - t * KT) * kRow4 + kch);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(Kh + (size_t)t * KT * kRow4),
                  "s"(ldsK + (unsigned)(buf * KT * kRow4)) : "memory");
@@ -424,42 +624,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) kf[s][hf] = *(const uint4 *)((const char *)&Ks[0][0] + (buf * KT + 32 * hf) * kRow4 + (kbase ^ (unsigned)(s << 4)));
   };
-  // ---- V: a thread's group of 32 codes of row vrow, or half of it
-  uint32_t vc[NV * 2], vs;
-  const int vrow = tid / (2 * WAVES / 2), vpart = tid % WAVES, vg = vpart * 4 / WAVES;
+  // ---- V: a thread's group of 32 codes of row vrow
+  uint4 vc;
+  uint32_t vs;
+  const int vrow = tid >> 2, vg = tid & 3;
   auto fetch_v = [&](int t) {
     const unsigned r = (unsigned)min(vrow, p.tokens - 1 - t * KT);
-    const uint8_t *at = Vh + (size_t)t * KT * kRow4;
-    if constexpr (WAVES == 4) {
-      const uint4 x = *(const uint4 *)(at + r * kRow4 + vpart * 16);
-      vc[0] = x.x; vc[1] = x.y; vc[2] = x.z; vc[3] = x.w;
-    } else {
-      const uint2 x = *(const uint2 *)(at + r * kRow4 + vpart * 8);
-      vc[0] = x.x; vc[1] = x.y;
-    }
+    vc = *(const uint4 *)(Vh + (size_t)t * KT * kRow4 + (r * kRow4 + vg * 16));
     vs = *(const uint32_t *)((const char *)(vsh + (size_t)t * KT) + 4u * r);
   };
   char *const vput = (char *)&Vs[0][0] + vrow * 256;
-  const unsigned vswz = (unsigned)(16 / WAVES * vpart ^ (vrow & 3) * 5) << 4;
+  const unsigned vswz = (unsigned)(4 * vg ^ (vrow & 3) * 5) << 4;
   auto put_v = [&](int buf, int k, float scale) {
-    *(uint4 *)(vput + buf * KT * 256 + (vswz ^ (unsigned)(k << 4))) = decode4_8(vc[k], scale);
+    const uint32_t w = k == 0 ? vc.x : k == 1 ? vc.y : k == 2 ? vc.z : vc.w;
+    *(uint4 *)(vput + buf * KT * 256 + (vswz ^ (unsigned)(k << 4))) = decode4_8(w, scale);
   };
   // A row that does not see a key gives it weight 0, and 0 x NaN is not 0: in tiles that only some rows see, groups of V
   // that are NaN stay out of the products and come back at the end for the rows that do see them.
   auto screen = [&](int t) {
     const bool bad = (vs >> (8 * vg) & 0xFFu) == kNanScale;
     const uint64_t who = __ballot(bad);
-    if (vpart == 0) {
-      uint32_t b = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) b |= (uint32_t)(who >> (lane + k * WAVES / 4) & 1ull) << k;
-      rowbad[(t - t_masked) * KT + vrow] = (uint8_t)b;
-    }
-    if (bad) {
-#pragma unroll
-      for (int k = 0; k < NV * 2; ++k) vc[k] = 0u;
-      vs = 0x7F7F7F7Fu;
-    }
+    if (vg == 0) rowbad[(t - t_masked) * KT + vrow] = (uint8_t)(who >> lane & 15ull);
+    if (bad) { vc = make_uint4(0u, 0u, 0u, 0u); vs = 0x7F7F7F7Fu; }
   };
   unsigned vbase;
   {
@@ -502,7 +688,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args
       {
         const float s = scale4(vs >> (8 * vg) & 0xFFu);
 #pragma unroll
-        for (int k = 0; k < NV * 2; ++k) put_v(0, k, s);
+        for (int k = 0; k < 4; ++k) put_v(0, k, s);
       }
       fetch_v(min(t_begin + 1, t_end - 1));
       for (int t = t_begin; t < t_end; ++t) {
@@ -523,13 +709,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args
         __builtin_amdgcn_sched_barrier(0);
 #define SA_STEP(S, I, K) \
         score_pair<S, I>(kf, r, e, ks); \
-        if constexpr ((K) < NV * 2) put_v(cur ^ 1, K, scale); \
+        if constexpr ((K) < 4) put_v(cur ^ 1, K, scale); \
         asm volatile("" : "+v"(e[0]), "+v"(e[1])); \
         __builtin_amdgcn_sched_barrier(0);
-        SA_STEP(0, 0, 0) SA_STEP(0, 1, 1)
-        if constexpr (kCodes > 2) { SA_STEP(0, kCodes - 1, 2) }
-        SA_STEP(1, 0, 3 - (kCodes < 3)) 
-        if constexpr (kCodes < 3) { SA_STEP(1, 1, 3) } else { SA_STEP(1, 1, 9) SA_STEP(1, kCodes - 1, 9) }
+        SA_STEP(0, 0, 0) SA_STEP(0, 1, 1) SA_STEP(0, 2, 2) SA_STEP(1, 0, 3) SA_STEP(1, 1, 4) SA_STEP(1, 2, 4)
 #undef SA_STEP
         fetch_v(min(t + 2, t_end - 1));
         if (kAgain) {
@@ -613,23 +796,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend4_rows_kernel(Attend4Args
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit, as for the 8-bit cache.
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 256; }
 
-// Splits: as many as give two workgroups a compute unit.
-struct Plan { bool few; int S; };
+struct Plan { int rows, S; };
 Plan plan_of(const Shape &sh, int rows, int tokens) {
-  const bool few = rows <= 64;
-  const int per = few ? kRowsFew : kRowsMany, keys = few ? 32 : 64;
+  const int per = rows <= kRowsStep ? kRowsStep : rows <= 64 ? kRowsFew : kRowsMany, keys = per == kRowsMany ? 64 : 32;
   const int64_t wgs = (rows + per - 1) / per * (int64_t)sh.Hkv, all = (int64_t)rows * sh.Hkv;
   const int tiles = (tokens + keys - 1) / keys;
   const int64_t top = std::min<int64_t>(std::min(tiles / 4 + 1, kMaxSplits), (int64_t)max_slots(sh) / all);
-  const int S = (int)std::max<int64_t>(1, std::min<int64_t>(2 * sh.n_cu / wgs, top)), share = (tiles + S - 1) / S;
-  return {few, (tiles + share - 1) / share};
+  const int S = (int)std::max<int64_t>(1, std::min<int64_t>((per == kRowsStep ? 4 : 2) * sh.n_cu / wgs, top)), share = (tiles + S - 1) / S;
+  return {per, (tiles + share - 1) / share};
 }
 
 }  // namespace
 
 void cache4_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits) {
   const Plan plan = plan_of(sh, sh.g * n, pos + n);
-  *rows = plan.few ? kRowsFew : kRowsMany;
+  *rows = plan.rows;
   *splits = plan.S;
 }
 
@@ -645,17 +826,18 @@ hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, 
   a.c = sh.scale * 1.4426950408889634f;
   const Plan plan = plan_of(sh, a.rows, a.tokens);
   a.S = plan.S;
-  a.tiles = (a.rows + (plan.few ? kRowsFew : kRowsMany) - 1) / (plan.few ? kRowsFew : kRowsMany);
+  a.tiles = (a.rows + plan.rows - 1) / plan.rows;
   const int64_t wgs = (int64_t)a.tiles * sh.Hkv;
   a.turn = a.tiles;
-  if (!plan.few && wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu) a.turn = std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S)));
+  if (plan.rows == kRowsMany && wgs * a.S > sh.n_cu && wgs * a.S <= 2 * sh.n_cu) a.turn = std::max(1, (int)(sh.n_cu / (sh.Hkv * a.S)));
   const int64_t all = (int64_t)a.rows * sh.Hkv;
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
   const unsigned grid = (unsigned)(wgs * a.S);
-  if (plan.few && a.rows <= 2 * kRowsFew) attend4_few_kernel<2><<<grid, kThreads, 0, st>>>(a);
-  else if (plan.few) attend4_few_kernel<1><<<grid, kThreads, 0, st>>>(a);
-  else attend4_rows_kernel<4><<<grid, 256, 0, st>>>(a);
+  if (plan.rows == kRowsStep) attend4_step_kernel<<<grid, kThreads, 0, st>>>(a);
+  else if (plan.rows == kRowsFew && a.rows <= 2 * kRowsFew) attend4_few_kernel<2><<<grid, kThreads, 0, st>>>(a);
+  else if (plan.rows == kRowsFew) attend4_few_kernel<1><<<grid, kThreads, 0, st>>>(a);
+  else attend4_rows_kernel<<<grid, kThreads, 0, st>>>(a);
   launch_join(a, all, st);
   return hipGetLastError();
 }
