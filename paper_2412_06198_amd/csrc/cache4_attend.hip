@@ -24,12 +24,26 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 constexpr int kRowsMany = 128, kRowsFew = 32, kRowsStep = 16;  // query rows of a workgroup
 constexpr int kCodes = 3;                      // of an element of Q
 
+// x / d for 0 <= x < 2^30 as a product: m = ceil(2^(31 + shift) / d) with 2^shift >= d is off by less than d of 2^(31 + shift).  (A division by a number
+// that is not known takes some 30 instructions, and what a short call waits for is its code, read once.)
+struct Divisor {
+  uint32_t m;
+  int shift;
+};
+__device__ inline int divided(int x, Divisor d) { return (int)(__umulhi(2u * (uint32_t)x, d.m) >> d.shift); }
+Divisor divisor(int d) {
+  int shift = 0;
+  while (1 << shift < d) ++shift;
+  return {(uint32_t)((((uint64_t)1 << (31 + shift)) + d - 1) / d), shift};
+}
+
 struct Attend4Args : AttendOut {
   const uint16_t *Q;
   const uint8_t *K, *V;
   const uint32_t *k_scale, *v_scale;  // a row's four bytes
   int64_t q_hs, q_rs, capacity;
   int tiles;         // row tiles
+  Divisor by_g, by_S;
   int turn;          // many rows: row tiles from the last one down, this many, then from the first one up
   int pos, tokens;   // of the first query; in the cache
   float c;           // softmax scale * log2(e), which goes into Q
@@ -67,6 +81,19 @@ __device__ inline uint32_t cut_query(const uint16_t *at, float c, i32x6 (&code)[
   }
   const uint32_t b = (uint32_t)(127 + e);
   return bits < 0x7F800000u ? b | (b - 4) << 8 | (b - 8) << 16 : 0x00FFFFFFu;
+}
+
+// A workgroup's KV head, split and row tile: KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then
+// splits, then row tiles.  A grid is at most 65535 deep; further row tiles stand beside the KV heads.
+struct Place { int kvh, sp, tile; };
+__device__ inline Place place_of(const Attend4Args &p) {
+  Place at = {(int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z};
+  for (; at.kvh >= p.Hkv; at.kvh -= p.Hkv) at.tile += gridDim.z;
+  return at;
+}
+dim3 grid_of(const Attend4Args &p) {
+  const int deep = std::min(p.tiles, 32768);
+  return dim3((unsigned)(p.Hkv * ((p.tiles + deep - 1) / deep)), (unsigned)p.S, (unsigned)deep);
 }
 
 template <int A_BYTE, int PART>
@@ -226,16 +253,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // KV heads side by side, then splits, then row tiles from the longest down
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = (p.tiles - 1 - rest / p.S) * kRowsFew;
-  const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
+  const Place at_grid = place_of(p);
+  if (at_grid.tile >= p.tiles) return;
+  const int kvh = at_grid.kvh, sp = at_grid.sp, r0 = (p.tiles - 1 - at_grid.tile) * kRowsFew;  // the longest row tiles first
+  const int seen_all = p.pos + divided(r0, p.by_g);     // last key that every row sees
   const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
-  const int n_tiles = (p.pos + (min(r0 + kRowsFew, p.rows) - 1) / p.g) / KT + 1;
-  const int per = (n_tiles + p.S - 1) / p.S;
+  const int n_tiles = (p.pos + divided(min(r0 + kRowsFew, p.rows) - 1, p.by_g)) / KT + 1;
+  const int per = divided(n_tiles + p.S - 1, p.by_S);
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
 
   // this lane's row, and the last key that it sees
-  const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
+  const int row = min(r0 + q, p.rows - 1), tok = divided(row, p.by_g), head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const size_t first = (size_t)kvh * p.capacity;
   const uint8_t *__restrict__ Kh = p.K + first * kRow4 + 32 * gg, *__restrict__ Vh = p.V + first * kRow4 + 16 * (lane & 3);
@@ -261,8 +289,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   // Q: the groups 2gg and 2gg + 1 of a row, as the lane's K
   i32x6 qc[2][kCodes];
   uint32_t qs[2];
+  const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg;
+#pragma unroll 1
+  for (int s = 0; s < 2; ++s) {  // one after the other, in half the code
 #pragma unroll
-  for (int s = 0; s < 2; ++s) qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, p.c, qc[s]);
+    for (int i = 0; i < kCodes; ++i) qc[0][i] = qc[1][i];
+    qs[0] = qs[1];
+    qs[1] = cut_query(qrow + 32 * s, p.c, qc[1]);
+  }
 
   f32x16 oacc[4];
 #pragma unroll
@@ -339,16 +373,17 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, b = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // KV heads side by side, then splits, then row tiles from the longest down
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, r0 = (p.tiles - 1 - rest / p.S) * ROWS;
-  const int seen_all = p.pos + r0 / p.g;     // last key that every row sees
+  const Place at_grid = place_of(p);
+  if (at_grid.tile >= p.tiles) return;
+  const int kvh = at_grid.kvh, sp = at_grid.sp, r0 = (p.tiles - 1 - at_grid.tile) * ROWS;  // the longest row tiles first
+  const int seen_all = p.pos + divided(r0, p.by_g);     // last key that every row sees
   const int t_masked = (seen_all + 1) / KT;  // first tile that some do not
-  const int n_tiles = (p.pos + (min(r0 + ROWS, p.rows) - 1) / p.g) / KT + 1;
-  const int per = (n_tiles + p.S - 1) / p.S;
+  const int n_tiles = (p.pos + divided(min(r0 + ROWS, p.rows) - 1, p.by_g)) / KT + 1;
+  const int per = divided(n_tiles + p.S - 1, p.by_S);
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
 
   // this lane's row, and the last key that it sees
-  const int row = min(r0 + q, p.rows - 1), tok = row / p.g, head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
+  const int row = min(r0 + q, p.rows - 1), tok = divided(row, p.by_g), head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const size_t first = (size_t)kvh * p.capacity;
   const uint8_t *__restrict__ Kh = p.K + first * kRow4 + 16 * b, *__restrict__ Vh = p.V + first * kRow4 + 16 * (lane & 3);
@@ -495,7 +530,7 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
     L += s_l[k][mr] * w[k];
   }
   const size_t slot = ((size_t)kvh * p.rows + orow) * p.S + sp;
-  const int otok = orow / p.g;
+  const int otok = divided(orow, p.by_g);
   uint16_t *o = p.O + (size_t)(kvh * p.g + orow - otok * p.g) * p.o_hs + (size_t)otok * p.o_rs;
   if (p.S > 1 && d0 == 0) p.ml[slot] = make_float2(M, L);
   const float inv = p.S > 1 ? 1.f : 1.f / L;
@@ -586,14 +621,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 
   const int tid = threadIdx.x, lane = tid & 63, q = lane & 31, gg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // KV heads side by side (workgroups go to the XCDs in turn: with 8 KV heads each stays in one L2), then splits, then row tiles
-  const int kvh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, sp = rest % p.S, down = rest / p.S;
-  const int rt = down < p.turn ? p.tiles - 1 - down : down - p.turn;
+  const Place at_grid = place_of(p);
+  if (at_grid.tile >= p.tiles) return;
+  const int kvh = at_grid.kvh, sp = at_grid.sp, rt = at_grid.tile < p.turn ? p.tiles - 1 - at_grid.tile : at_grid.tile - p.turn;
   const int r0 = rt * ROWS, r_last = min(r0 + ROWS, p.rows) - 1;
-  const int seen_all = p.pos + r0 / p.g;                // last key that every row of the workgroup sees
+  const int seen_all = p.pos + divided(r0, p.by_g);                // last key that every row of the workgroup sees
   const int t_masked = (seen_all + 1) / KT;             // first tile that some do not
-  const int n_tiles = (p.pos + r_last / p.g) / KT + 1;  // tiles that some row sees
-  const int per = (n_tiles + p.S - 1) / p.S;
+  const int n_tiles = (p.pos + divided(r_last, p.by_g)) / KT + 1;  // tiles that some row sees
+  const int per = divided(n_tiles + p.S - 1, p.by_S);
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
 
   const size_t first = (size_t)kvh * p.capacity;
@@ -665,12 +700,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   {
     const int lo = min(r0 + 32 * wave, p.rows - 1);
     r.row = min(lo + q, p.rows - 1);
-    tok = r.row / p.g;
+    tok = divided(r.row, p.by_g);
     head = kvh * p.g + (r.row - tok * p.g);
     r.see = p.pos + tok;
-    r.all = p.pos + lo / p.g;
+    r.all = p.pos + divided(lo, p.by_g);
+    const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg;
+#pragma unroll 1
+    for (int s = 0; s < 2; ++s) {  // one after the other, in half the code
 #pragma unroll
-    for (int s = 0; s < 2; ++s) r.qs[s] = cut_query(p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg + 32 * s, p.c, r.qc[s]);
+      for (int i = 0; i < kCodes; ++i) r.qc[0][i] = r.qc[1][i];
+      r.qs[0] = r.qs[1];
+      r.qs[1] = cut_query(qrow + 32 * s, p.c, r.qc[1]);
+    }
   }
   f32x16 oacc[4];
   f32x4 lacc[2];
@@ -833,7 +874,9 @@ hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, 
   const int64_t all = (int64_t)a.rows * sh.Hkv;
   a.ml = (float2 *)scratch;
   a.part = (float *)((char *)scratch + max_slots(sh) * 8);
-  const unsigned grid = (unsigned)(wgs * a.S);
+  a.by_g = divisor(a.g);
+  a.by_S = divisor(a.S);
+  const dim3 grid = grid_of(a);
   if (plan.rows == kRowsStep) attend4_step_kernel<<<grid, kThreads, 0, st>>>(a);
   else if (plan.rows == kRowsFew && a.rows <= 2 * kRowsFew) attend4_few_kernel<2><<<grid, kThreads, 0, st>>>(a);
   else if (plan.rows == kRowsFew) attend4_few_kernel<1><<<grid, kThreads, 0, st>>>(a);
