@@ -19,6 +19,7 @@ namespace sa {
 namespace {
 
 typedef int i32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 constexpr int kRowsMany = 128, kRowsFew = 32, kRowsStep = 16;  // query rows of a workgroup
@@ -588,9 +589,8 @@ template <int N, int COUNT>
 __device__ inline void probabilities(f32x16 (&e)[2], u32x4 (&pb)[4]) {
 #pragma unroll
   for (int n = N; n < N + COUNT; ++n) {
-    const float a = __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7)]), b = __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7) + 1]);
-    const bf16x2 pr = {(__bf16)a, (__bf16)b};
-    pb[n >> 2][n & 3] = __builtin_bit_cast(uint32_t, pr);
+    const f32x2 x = {__builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7)]), __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7) + 1])};
+    pb[n >> 2][n & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
   }
 }
 
@@ -635,21 +635,30 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   const uint8_t *__restrict__ Kh = p.K + first * kRow4, *__restrict__ Vh = p.V + first * kRow4;
   const uint32_t *__restrict__ ksh = p.k_scale + first, *__restrict__ vsh = p.v_scale + first;
 
-  // ---- K: 64 rows of 64 bytes, the 16-byte chunk c of row r in place c ^ (r / 4) % 4, so that b128 reads of 16 rows hit 64 banks (the
-  // lane that owns place x of row r reads chunk x ^ (r / 4) % 4).  Behind the tokens the last row again, here and below: nobody sees it there.
+  // ---- what a thread reads of a tile, from the tile's first byte on; behind the tokens the last row again: nobody sees it there.
+  // K: 64 rows of 64 bytes, the 16-byte chunk c of row r in place c ^ (r / 4) % 4, so that b128 reads of 16 rows hit 64 banks (the
+  // lane that owns place x of row r reads chunk x ^ (r / 4) % 4).  V: a group of 32 codes of row vrow.  Scales of K: of the keys q and q + 32.
   const unsigned ldsK = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)&Ks[0][0] + wave * 1024;
-  const int krow = 16 * wave + (lane >> 2), kch = ((lane & 3) ^ (lane >> 4)) << 4;
+  const int vrow = tid >> 2, vg = tid & 3;
+  unsigned k_at, v_at, vs_at, ks_at[2];
+  auto offsets = [&](int rows) {
+    k_at = (unsigned)(min(16 * wave + (lane >> 2), rows - 1) * kRow4 + (((lane & 3) ^ (lane >> 4)) << 4));
+    const int r = min(vrow, rows - 1);
+    v_at = (unsigned)(r * kRow4 + vg * 16);
+    vs_at = 4u * (unsigned)r;
+    ks_at[0] = 4u * (unsigned)min(q, rows - 1);
+    ks_at[1] = 4u * (unsigned)min(q + 32, rows - 1);
+  };
+  const int n_whole = p.tokens / KT;  // tiles without a row behind the tokens
   auto issue_k = [&](int t, int buf) {
-    const unsigned at = (unsigned)(min(krow, p.tokens - 1 - t * KT) * kRow4 + kch);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(Kh + (size_t)t * KT * kRow4),
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(k_at), "s"(Kh + (size_t)t * KT * kRow4),
                  "s"(ldsK + (unsigned)(buf * KT * kRow4)) : "memory");
   };
-  uint32_t kn[2], ks[2];  // scales of the keys q and q + 32, as read and as the products take them
+  uint32_t kn[2], ks[2];  // as read, and as the products take them
   auto fetch_ks = [&](int t) {
-    const uint32_t *at = ksh + (size_t)t * KT;
-    const int lim = p.tokens - 1 - t * KT;
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) kn[hf] = *(const uint32_t *)((const char *)at + 4u * (unsigned)min(q + 32 * hf, lim));
+    const char *at = (const char *)(ksh + (size_t)t * KT);
+    kn[0] = *(const uint32_t *)(at + ks_at[0]);
+    kn[1] = *(const uint32_t *)(at + ks_at[1]);
   };
   const unsigned kbase = (unsigned)(q * kRow4) | (unsigned)(((2 * gg) ^ (q >> 2 & 3)) << 4);
   uint4 kf[2][2];  // [d-slab][half of the keys]
@@ -659,14 +668,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) kf[s][hf] = *(const uint4 *)((const char *)&Ks[0][0] + (buf * KT + 32 * hf) * kRow4 + (kbase ^ (unsigned)(s << 4)));
   };
-  // ---- V: a thread's group of 32 codes of row vrow
   uint4 vc;
   uint32_t vs;
-  const int vrow = tid >> 2, vg = tid & 3;
   auto fetch_v = [&](int t) {
-    const unsigned r = (unsigned)min(vrow, p.tokens - 1 - t * KT);
-    vc = *(const uint4 *)(Vh + (size_t)t * KT * kRow4 + (r * kRow4 + vg * 16));
-    vs = *(const uint32_t *)((const char *)(vsh + (size_t)t * KT) + 4u * r);
+    vc = *(const uint4 *)(Vh + (size_t)t * KT * kRow4 + v_at);
+    vs = *(const uint32_t *)((const char *)(vsh + (size_t)t * KT) + vs_at);
   };
   char *const vput = (char *)&Vs[0][0] + vrow * 256;
   const unsigned vswz = (unsigned)(4 * vg ^ (vrow & 3) * 5) << 4;
@@ -690,6 +696,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
   auto begin = [&] {
+    offsets(t_begin < n_whole ? KT : p.tokens - t_begin * KT);
     issue_k(t_begin, 0);
     fetch_v(t_begin);
     fetch_ks(t_begin);
@@ -731,9 +738,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 #pragma unroll
         for (int k = 0; k < 4; ++k) put_v(0, k, s);
       }
-      fetch_v(min(t_begin + 1, t_end - 1));
-      for (int t = t_begin; t < t_end; ++t) {
-        const int cur = (t - t_begin) & 1, j0 = t * KT, next = min(t + 1, t_end - 1);
+      if (t_begin + 1 < t_end) {
+        if (t_begin + 1 >= n_whole) offsets(p.tokens - (t_begin + 1) * KT);
+        fetch_v(t_begin + 1);
+      }
+      auto tile = [&](auto CUR, int t) {
+        constexpr int cur = decltype(CUR)::value;
+        const int j0 = t * KT;
         // K of this tile has landed, and V of the next one; after the barrier both buffers of the tile hold it and
         // every wave is done with the tile before
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
@@ -741,9 +752,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         read_k(cur);
         ks[0] = kn[0] >> (16 * gg);
         ks[1] = kn[1] >> (16 * gg);
-        issue_k(next, cur ^ 1);
-        fetch_ks(next);
-        if (t + 1 >= t_masked && t + 1 < t_end) screen(t + 1);
+        if (t + 1 < t_end) {
+          issue_k(t + 1, cur ^ 1);
+          fetch_ks(t + 1);
+          if (t + 1 >= t_masked) screen(t + 1);
+        }
         const float scale = scale4(vs >> (8 * vg) & 0xFFu);
         // S^T = K Q^T; beside it V of the next tile becomes bf16 (behind the last tile what is left in the registers: nobody reads it)
         f32x16 e[2];
@@ -755,7 +768,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         __builtin_amdgcn_sched_barrier(0);
         SA_STEP(0, 0, 0) SA_STEP(0, 1, 1) SA_STEP(0, 2, 2) SA_STEP(1, 0, 3) SA_STEP(1, 1, 4) SA_STEP(1, 2, 4)
 #undef SA_STEP
-        fetch_v(min(t + 2, t_end - 1));
+        if (t + 2 < t_end) {
+          if (t + 2 >= n_whole) offsets(p.tokens - (t + 2) * KT);  // K and its scales follow
+          fetch_v(t + 2);
+        }
         if (kAgain) {
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
@@ -793,9 +809,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         step(Int<0>()); step(Int<1>()); step(Int<2>()); step(Int<3>()); step(Int<4>()); step(Int<5>()); step(Int<6>()); step(Int<7>());
         step(Int<8>()); step(Int<9>()); step(Int<10>()); step(Int<11>()); step(Int<12>()); step(Int<13>()); step(Int<14>()); step(Int<15>());
         __builtin_amdgcn_s_setprio(0);
+      };
+      for (int t = t_begin; t < t_end; t += 2) {
+        tile(Int<0>(), t);
+        if (t + 1 < t_end) tile(Int<1>(), t + 1);
       }
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): K of a tile behind the last has landed, before its LDS is another's
     r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
   };
   run(Int<0>());
@@ -807,7 +826,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   const bool good = r.see < t_begin * KT || (r.l > 0x1p-80f && r.l < 0x1p100f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f);
   if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!good)) && t_begin < t_end) {
     float top = -INFINITY;
+    offsets(t_begin < n_whole ? KT : p.tokens - t_begin * KT);
     for (int t = t_begin; t < t_end; ++t) {
+      if (t >= n_whole) offsets(p.tokens - t * KT);
       __syncthreads();
       issue_k(t, 0);
       fetch_ks(t);
