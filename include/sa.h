@@ -396,11 +396,13 @@ sa_status sa_cache4_read(sa_ctx *ctx, const sa_cache4 *cache, sa_rows K, sa_rows
 /* sa_cache_decode on this cache: same index, same kept keys, same q, o and pos, same use of ctx's workspace. */
 sa_status sa_cache4_decode(sa_ctx *ctx, const sa_cache4 *cache, const void *q, sa_index idx, int64_t pos, void *o, void *hip_stream);
 
-/* sa_cache_attend on this cache: same Q, O, n, pos and scratch (sa_cache_attend_scratch_bytes), same limits and roundings.  Scores take
- * an element of Q, times the softmax scale, to 2^-12.8 of the largest of its group of 32 or better. */
+/* sa_cache_attend on this cache: same Q, O, n, pos and scratch (sa_cache_attend_scratch_bytes), same limits.  Scores, sums and statistics are fp32 and the
+ * output is rounded to bf16 once.  Scores take an element of Q, times the softmax scale, to 2^-12.8 of the largest of its group of 32 or
+ * better; probabilities are multiplied to 2^-15 of themselves, but rounded to bf16 where sa_cache4_attend_plan says 128 rows, or 32 with more than 64
+ * query rows a KV head (n * n_q_heads / n_kv_heads). */
 sa_status sa_cache4_attend(sa_ctx *ctx, const sa_cache4 *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
                            void *scratch_dev, size_t scratch_bytes, void *hip_stream);
-/* sa_cache_attend_plan of such a call. */
+/* How such a call is carried out, as sa_cache_attend_plan: a workgroup takes 16, 32 or 128 query rows, of three kernels. */
 sa_status sa_cache4_attend_plan(const sa_ctx *ctx, int64_t n, int64_t pos, int32_t *rows, int32_t *splits);
 
 const char *sa_last_error(const sa_ctx *ctx);

@@ -858,20 +858,51 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit, as for the 8-bit cache.
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 256; }
 
+// Which kernel, and into how many splits the keys go: the least of an estimate over the three kernels and over splits that fill a quarter of the card, a
+// half, .. all that a compute unit holds at once.  The terms were fitted (us, logarithms) to 3400 measurements of 350 drawn shapes of 4 to 64
+// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 1.2 % slower than the best of all kernels and splits in the
+// mean, and 16 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
+//                                              16 rows   32 rows   128 rows
+//   start and end                              3.85      5.8       5.8
+//   keys of a round of a workgroup's waves     128       128       64
+//   a round, up to a workgroup a compute unit  0.9       0.7       0.91
+//   more of that for each further one          0.3       0.58      0.47
+//   more at the start for each further one     1.3
+//   workgroups a compute unit at once          4         2         2
+//   more than that: their number times this, of which rows see less than the longest one, and 0.6 of a start
+//   a join: its launch 2.9, and 1 KB written and read for each row and split
 struct Plan { int rows, S; };
-Plan plan_of(const Shape &sh, int rows, int tokens) {
-  const int per = rows <= kRowsStep ? kRowsStep : rows <= 64 ? kRowsFew : kRowsMany, keys = per == kRowsMany ? 64 : 32;
-  const int64_t wgs = (rows + per - 1) / per * (int64_t)sh.Hkv, all = (int64_t)rows * sh.Hkv;
-  const int tiles = (tokens + keys - 1) / keys;
-  const int64_t top = std::min<int64_t>(std::min(tiles / 4 + 1, kMaxSplits), (int64_t)max_slots(sh) / all);
-  const int S = (int)std::max<int64_t>(1, std::min<int64_t>((per == kRowsStep ? 4 : 2) * sh.n_cu / wgs, top)), share = (tiles + S - 1) / S;
-  return {per, (tiles + share - 1) / share};
+Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
+  struct Kernel { int rows, keys, waves, most; float start, more_start, round, more_round; };  // keys of a tile, waves that share out the tiles
+  const Kernel kernels[3] = {{kRowsStep, 32, 4, 4, 3.85f, 1.3f, 0.9f, 0.3f}, {kRowsFew, 32, 4, 2, 5.8f, 0.f, 0.7f, 0.58f}, {kRowsMany, 64, 1, 2, 5.8f, 0.f, 0.91f, 0.47f}};
+  const float mean = 0.5f + 0.5f * pos / tokens;  // keys that a row sees, against all
+  const int64_t all = (int64_t)rows * sh.Hkv;
+  Plan best = {kRowsStep, 1};
+  float least = INFINITY;
+  for (const Kernel &k : kernels) {
+    const int64_t wgs = (rows + k.rows - 1) / k.rows * (int64_t)sh.Hkv;
+    const int tiles = (tokens + k.keys - 1) / k.keys;
+    const int top = (int)std::min<int64_t>(std::min(tiles / k.waves + 1, kMaxSplits), std::max<int64_t>(1, (int64_t)max_slots(sh) / all));
+    for (int quarters : {0, 1, 2, 3, 4, 6, 8, 12, 16}) {  // of a workgroup a compute unit; 0: no splits
+      const int64_t fill = quarters * (int64_t)sh.n_cu / (4 * wgs);
+      if (quarters > 4 * k.most || (quarters > 0 && fill <= 1)) continue;
+      const int S0 = (int)std::max<int64_t>(1, std::min<int64_t>(fill, top));
+      const int share = (tiles + S0 - 1) / S0, S = (tiles + share - 1) / share, per = (share + k.waves - 1) / k.waves;
+      const float load = (float)wgs * S / sh.n_cu, beside = std::min(std::max(load - 1.f, 0.f), k.most - 1.f);
+      const float body = k.more_start * beside + per * (k.round + k.more_round * beside);
+      float t = k.start + body;
+      if (load > k.most) t = std::max(t, load / k.most * (0.6f * k.start + k.more_start * beside + per * (k.round + k.more_round * beside) * mean));
+      if (S > 1) t += 2.9f + all * S * 0.0003f;
+      if (t < least) { least = t; best = {k.rows, S}; }
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
 void cache4_attend_plan(const Shape &sh, int n, int pos, int *rows, int *splits) {
-  const Plan plan = plan_of(sh, sh.g * n, pos + n);
+  const Plan plan = plan_of(sh, sh.g * n, pos + n, pos);
   *rows = plan.rows;
   *splits = plan.S;
 }
@@ -886,7 +917,7 @@ hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, 
   a.g = sh.g; a.Hkv = sh.Hkv; a.rows = sh.g * n;
   a.pos = pos; a.tokens = pos + n;
   a.c = sh.scale * 1.4426950408889634f;
-  const Plan plan = plan_of(sh, a.rows, a.tokens);
+  const Plan plan = plan_of(sh, a.rows, a.tokens, pos);
   a.S = plan.S;
   a.tiles = (a.rows + plan.rows - 1) / plan.rows;
   const int64_t wgs = (int64_t)a.tiles * sh.Hkv;

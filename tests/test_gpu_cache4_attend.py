@@ -33,7 +33,7 @@ def _reference(q, keys, vals, pos, rows, scale=128.0 ** -0.5):
     hq, n, g = q.shape[0], q.shape[1], q.shape[0] // keys.shape[0]
     o, tol = np.empty(q.shape), np.empty(q.shape)
     later = np.arange(pos + n)[None] > pos + np.arange(n)[:, None]
-    of_p = 2.0 ** -15 if g * n <= 64 and rows < 128 else 2.0 ** -8
+    of_p = 2.0 ** -15 if rows == 16 or (rows == 32 and g * n <= 64) else 2.0 ** -8
     for h in range(hq):
         s = q[h] @ keys[h // g].T * scale
         s[later] = -np.inf
