@@ -5,7 +5,9 @@
 // bit of mantissa it is the scale that has to follow the values; a row's own scales make a token independent of its neighbours, so there
 // is no open block and a token may be written again.  x / s and code * s are exact, the rounding to the code is the only one.
 // Both directions read and write everything once: the bound is HBM.  A row is taken by 16 lanes, 8 elements each, so that every access of
-// a wave is contiguous (16 bytes a lane in bf16, 4 in codes); a group is four lanes, whose largest magnitude is two lane moves.
+// a wave is contiguous (16 bytes a lane in bf16, 4 in codes); a group is four lanes, whose largest magnitude is two lane moves.  128K tokens of 8 heads, 680 MB: 110 us
+// to append, 109 to read back (6.2 TB/s; a device copy moves 5.1), 128 to read back from 8 bits (6.3 TB/s).  What is read back goes past the caches
+// (120 us with ordinary stores), the codes do not, since they are read next (10K tokens stored and read back 19.5 us, 21.0 past them).
 #include "cache4_codes.h"
 #include "cache_codes.h"
 #include "sa_internal.h"
@@ -15,7 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = kThreads / 16;  // rows that a workgroup takes at a time
-constexpr int U = 4;                  // times, all reads of which are on their way at once
+constexpr int U = 2;                  // times, all reads of which are on their way at once (4: 128K tokens appended in 116 us instead of 110, read back in 120, 109; 1: 114, 123)
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -30,7 +32,7 @@ struct Append4Args {
 template <int CTRL>
 __device__ inline uint32_t row_moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
 
-// Grid (ceil(n / 64), KV heads, K or V).
+// Grid (ceil(n / 32), KV heads, K or V).
 __global__ __launch_bounds__(kThreads) void append4_kernel(Append4Args p) {
   const int side = blockIdx.z, h = blockIdx.y, ln = threadIdx.x & 15;
   const int64_t t0 = (int64_t)blockIdx.x * (kRows * U) + (threadIdx.x >> 4);
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void append4_kernel(Append4Args p) {
     word |= row_moved<0x124>(word);  // of the lanes 4 and 8 further round the row
     word |= row_moved<0x128>(word);
     const int64_t row = h * p.capacity + p.pos + t;
-    __builtin_nontemporal_store(codes, (uint32_t *)(p.codes[side] + row * kRow4 + ln * 4));
+    *(uint32_t *)(p.codes[side] + row * kRow4 + ln * 4) = codes;
     if (ln == 0) p.scale[side][row] = word;
   }
 }
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs p) {
       const float s = __uint_as_float(y[u][2]);
       y[u] = u32x4{decode2<TYPE, false>(y[u][0], s), decode2<TYPE, true>(y[u][0], s), decode2<TYPE, false>(y[u][1], s), decode2<TYPE, true>(y[u][1], s)};
     }
-    *(u32x4 *)(dst + t * p.rs[side]) = y[u];
+    __builtin_nontemporal_store(y[u], (u32x4 *)(dst + t * p.rs[side]));
   }
 }
 

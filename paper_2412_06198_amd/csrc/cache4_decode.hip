@@ -1,6 +1,8 @@
 // One decode step over the prefill index, K and V out of the 4-bit cache: the keys, their order and the launch are those of the step
 // over the 8-bit cache (cache_decode.hip), half the bytes.  A key is read by 16 lanes as 64 bytes of codes of K and of V, and the two bytes of
-// their group's scales, which the conversion to fp32 applies.  There is no open block, so all keys are rows of one kind.
+// their group's scales, which the conversion to fp32 applies.  There is no open block, so all keys are rows of one kind.  The bound is a launch and the
+// round trips to memory that follow one another, as there: 8 heads at 4K tokens 7.0 us with the host's call, 32 heads at 128K tokens, 3 % kept,
+// 11.1.
 #include <algorithm>
 
 #include "cache4_codes.h"
@@ -25,8 +27,8 @@ struct Cache4DecArgs {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kLanes = 16, kSlots = 64 / kLanes;  // lanes of a key, keys that a wave reads at once
-// Rows of K and of V that a lane has in flight per step.  2: up to 0.4 us faster on short lists, up to 2 slower on long ones;
-// 8 lanes a key with 16 bytes each: 3 % faster at 32 heads and 128K tokens, 0.1 to 0.8 us slower elsewhere.
+// Rows of K and of V that a lane has in flight per step.  8: 0.1 to 0.7 us slower from 4K tokens on, 2: up to 0.9.  8 lanes a key, 8 bytes
+// each: 0.2 us faster at 32 heads and 128K tokens, 0.1 to 0.6 slower elsewhere.
 constexpr int U = 4;
 constexpr int kStep = kSlots * U;
 constexpr int kRing = 128;                        // keys of a wave that are resolved and not yet read: 15 + 64 at most
@@ -265,9 +267,9 @@ __global__ __launch_bounds__(kThreads) void cache4_decode_kernel(Cache4DecArgs p
   if (s_last) merge<true>(part, L.n, wgt, &s_L, so[0], p.o + (size_t)h * kHeadDim);
 }
 
-// Partials of a head: three workgroups of four waves a compute unit in all.  Two, as in the step on bf16 tensors, are 5 %
-// slower with 32 heads (128K tokens 12.4 us instead of 11.5), four 12 % (4K tokens 8.3 instead of 7.1).
-int splits(const Shape &sh) { return std::max(2, std::min(64, 768 / sh.Hq)); }
+// Partials of a head: two workgroups of four waves a compute unit in all.  Three: 32 heads at 16K tokens and a tenth kept 8.9 us instead of 7.8, at
+// 4K and a fifth 9.9 instead of 8.6 (at 128K 10.9 instead of 11.1); one and a half: 8.5, 9.6, 12.4.
+int splits(const Shape &sh) { return std::max(2, std::min(64, 512 / sh.Hq)); }
 
 }  // namespace
 
