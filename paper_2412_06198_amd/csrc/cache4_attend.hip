@@ -720,10 +720,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
       r.qs[1] = cut_query(qrow + 32 * s, p.c, r.qc[1]);
     }
   }
+  const bool idle = r0 + 32 * wave >= p.rows;  // a wave without rows only turns its part of V into bf16
   f32x16 oacc[4];
   f32x4 lacc[2];
   // Probabilities are 2^e as it is: fp32 and bf16 hold them from 2^-126 to 2^127, so that nothing has to be searched, subtracted or rescaled.  Where
-  // that was too little (a row's sum beyond 2^100 or below 2^-80, an output that is no number) the workgroup looks for the rows' largest exponents
+  // that was too little (a row's sum beyond 2^100, or below 2^-20, where small values of V times small probabilities would leave fp32, or an
+  // output that is no number) the workgroup looks for the rows' largest exponents
   // and starts anew, with them subtracted.
   r.m = 0.f;
   auto run = [&](auto AGAIN) {
@@ -738,15 +740,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 #pragma unroll
         for (int k = 0; k < 4; ++k) put_v(0, k, s);
       }
-      if (t_begin + 1 < t_end) {
-        if (t_begin + 1 >= n_whole) offsets(p.tokens - (t_begin + 1) * KT);
-        fetch_v(t_begin + 1);
-      }
-      auto tile = [&](auto CUR, int t) {
-        constexpr int cur = decltype(CUR)::value;
-        const int j0 = t * KT;
-        // K of this tile has landed, and V of the next one; after the barrier both buffers of the tile hold it and
-        // every wave is done with the tile before
+      // What a tile begins with, for every wave: K of it has landed, and V of the next one; after the barrier both buffers of the tile hold it
+      // and every wave is done with the tile before.  The scale of V of the next tile.
+      auto turn = [&](int t, int cur) {
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
         __syncthreads();
         read_k(cur);
@@ -757,7 +753,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
           fetch_ks(t + 1);
           if (t + 1 >= t_masked) screen(t + 1);
         }
-        const float scale = scale4(vs >> (8 * vg) & 0xFFu);
+        return scale4(vs >> (8 * vg) & 0xFFu);
+      };
+      auto fetch_next = [&](int t) {
+        if (t >= t_end) return;
+        if (t >= n_whole) offsets(p.tokens - t * KT);  // K and its scales follow
+        fetch_v(t);
+      };
+      fetch_next(t_begin + 1);
+      auto tile = [&](auto CUR, int t) {
+        constexpr int cur = decltype(CUR)::value;
+        const int j0 = t * KT;
+        const float scale = turn(t, cur);
         // S^T = K Q^T; beside it V of the next tile becomes bf16 (behind the last tile what is left in the registers: nobody reads it)
         f32x16 e[2];
         __builtin_amdgcn_sched_barrier(0);
@@ -768,10 +775,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         __builtin_amdgcn_sched_barrier(0);
         SA_STEP(0, 0, 0) SA_STEP(0, 1, 1) SA_STEP(0, 2, 2) SA_STEP(1, 0, 3) SA_STEP(1, 1, 4) SA_STEP(1, 2, 4)
 #undef SA_STEP
-        if (t + 2 < t_end) {
-          if (t + 2 >= n_whole) offsets(p.tokens - (t + 2) * KT);  // K and its scales follow
-          fetch_v(t + 2);
-        }
+        fetch_next(t + 2);
         if (kAgain) {
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
@@ -810,9 +814,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         step(Int<8>()); step(Int<9>()); step(Int<10>()); step(Int<11>()); step(Int<12>()); step(Int<13>()); step(Int<14>()); step(Int<15>());
         __builtin_amdgcn_s_setprio(0);
       };
-      for (int t = t_begin; t < t_end; t += 2) {
-        tile(Int<0>(), t);
-        if (t + 1 < t_end) tile(Int<1>(), t + 1);
+      if (idle) {
+        for (int t = t_begin; t < t_end; ++t) {
+          const int cur = (t - t_begin) & 1;
+          const float scale = turn(t, cur);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) put_v(cur ^ 1, k, scale);
+          fetch_next(t + 2);
+        }
+      } else {
+        for (int t = t_begin; t < t_end; t += 2) {
+          tile(Int<0>(), t);
+          if (t + 1 < t_end) tile(Int<1>(), t + 1);
+        }
       }
     }
     r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
@@ -823,7 +837,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   for (int k = 0; k < 16; ++k)
 #pragma unroll
     for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
-  const bool good = r.see < t_begin * KT || (r.l > 0x1p-80f && r.l < 0x1p100f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f);
+  const bool good = idle || r.see < t_begin * KT || (r.l > 0x1p-20f && r.l < 0x1p100f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f);
   if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!good)) && t_begin < t_end) {
     float top = -INFINITY;
     offsets(t_begin < n_whole ? KT : p.tokens - t_begin * KT);
