@@ -370,7 +370,8 @@ sa_status sa_cache_read(sa_ctx *ctx, const sa_cache *cache, int64_t tokens, sa_r
 /* ---- the cache in 4 bits -----------------------------------------------------------------------------
  * DEVICE buffers owned by the caller, 136 bytes for a token and KV head (8 bits: 256, bf16: 512).  A row (a token of a KV head) has four
  * groups of 32 adjacent elements; a group has 32 codes of OCP e2m1 (a sign, and 0 0.5 1 1.5 2 3 4 6) and one scale 2^e, kept as the byte e + 127
- * (OCP E8M0).  A key is code * 2^e, exactly a bf16 value; a group whose byte is 255 is NaN.  There are no blocks: a token stands by itself, may
+ * (OCP E8M0): bytes 27 .. 252 (e from -100 to 125), or 255 for a group that is NaN; others are not read as the type would have them.  A key is
+ * code * 2^e, exactly a bf16 value.  There are no blocks: a token stands by itself, may
  * be taken back and written again, and what stands behind the tokens is never read.
  *   k, v              [n_kv_heads][capacity][64]  codes, element 2i of a row in the lower half of byte i
  *   k_scale, v_scale  [n_kv_heads][capacity][4]   scale bytes
@@ -399,7 +400,7 @@ sa_status sa_cache4_decode(sa_ctx *ctx, const sa_cache4 *cache, const void *q, s
 /* sa_cache_attend on this cache: same Q, O, n, pos and scratch (sa_cache_attend_scratch_bytes), same limits.  Scores, sums and statistics are fp32 and the
  * output is rounded to bf16 once.  Scores take an element of Q, times the softmax scale, to 2^-12.8 of the largest of its group of 32 or
  * better; probabilities are multiplied to 2^-15 of themselves, but rounded to bf16 where sa_cache4_attend_plan says 128 rows, or 32 with more than 64
- * query rows a KV head (n * n_q_heads / n_kv_heads). */
+ * query rows a KV head (n * n_q_heads / n_kv_heads).  A row's sum of values is infinite or NaN where 2^8 * (its tokens) * max|V| leaves fp32. */
 sa_status sa_cache4_attend(sa_ctx *ctx, const sa_cache4 *cache, sa_rows Q, int64_t n, int64_t pos, sa_rows O,
                            void *scratch_dev, size_t scratch_bytes, void *hip_stream);
 /* How such a call is carried out, as sa_cache_attend_plan: a workgroup takes 16, 32 or 128 query rows, of three kernels. */

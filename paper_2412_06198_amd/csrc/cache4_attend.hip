@@ -1,13 +1,14 @@
-// Causal attention of the newest n tokens over the 4-bit cache: O = softmax(scale Q K^T) V, row by row, with the running maximum and sum of an
-// online softmax, for n from one token to thousands.  The rows, tiles and splits are those of the 8-bit cache (cache_attend.hip); what the 4 bits
-// change is that K goes into the products as it is: its codes and scales are the operands of the scaled matrix instructions, and
-// a group of 32 elements is what a lane holds of one.
+// Causal attention of the newest n tokens over the 4-bit cache: O = softmax(scale Q K^T) V, row by row, for n from one token to thousands.  The rows,
+// tiles and splits are those of the 8-bit cache (cache_attend.hip); what the 4 bits change is that K goes into the products as it
+// is: its codes and scales are the operands of the scaled matrix instructions, and a group of 32 elements is what a lane holds of one.
 //   Q, times the softmax scale and log2(e) in fp32, becomes the sum of three codes of 6 bits (e2m3), scales 2^e, 2^(e - 4), 2^(e - 8) for a group of
 //   32, the least e with every magnitude <= 7.5 2^e: each takes what the ones before leave, and what the last leaves is 2^-10.9 scales
 //   at most, 2^-12.8 of the group's largest.  Codes of 4 and 6 bits multiply at twice the rate of 8 and four times that of 16, so three of them cost
-//   three quarters of two codes of 8 bits or of one product in bf16.
-//   The products start at minus the row's reference in place of 0: what comes out is the exponent of a probability.
+//   three quarters of two codes of 8 bits or of one product in bf16.  (Two codes: chunks 8 % faster, but scores off by 1.4e-3 in the mean.)
 //   V has to be multiplied with probabilities, which need bf16: its codes are turned into bf16 on their way into LDS.
+// Three kernels, for 16, 32 and 128 query rows a workgroup, and a join of a row's splits; plan_of says which one a call takes.  The first two keep the
+// running maximum and sum of an online softmax; with 32 rows the products start at minus a row's reference, so that what comes out is
+// the exponent of a probability; with 128 rows probabilities are 2^exponent as it is, and rows that this does not fit are done once more.
 #include <algorithm>
 #include <cmath>
 
@@ -23,7 +24,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 constexpr int kRowsMany = 128, kRowsFew = 32, kRowsStep = 16;  // query rows of a workgroup
-constexpr int kCodes = 3;                      // of an element of Q
+constexpr int kCodes = 3;                                      // of an element of Q
 
 // x / d for 0 <= x < 2^30 as a product: m = ceil(2^(31 + shift) / d) with 2^shift >= d is off by less than d of 2^(31 + shift).  (A division by a number
 // that is not known takes some 30 instructions, and what a short call waits for is its code, read once.)
@@ -104,107 +105,81 @@ __device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[kCodes], 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 2, A_BYTE, (int)k_scale, PART, (int)q_scale);
 }
 
-// A tile's exponents (lane = row, accumulator r of half hf <-> key 32hf + 8(r/4) + 4gg + r%4 of HF * 32) into a row's running softmax and its outputs.
+// A tile's exponents (lane = row, accumulator r <-> key 8(r/4) + 4gg + r%4 of 32) into a row's running softmax and its outputs.
 // They are relative to the row's reference m_run, or to 0 before it has one; start: what the next products begin with.
 // masked: keys from place lim + 1 (less 4gg) on are not seen.
-// PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each; 2: a leading part and the rest, 2^-15, by twice
+// PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each; 2: a leading part, cut, and the rest, 2^-15, by twice
 // the products.  launch_cache4_attend says which.
-template <int PARTS, int HF>
-__device__ inline void absorb_exponents(f32x16 (&sacc)[HF], bool masked, int lim, const uint16_t *Vt, unsigned vbase,
+template <int PARTS>
+__device__ inline void absorb_exponents(f32x16 &e, bool masked, int lim, const uint16_t *Vt, unsigned vbase,
                                         float &m_run, f32x16 &start, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
   typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
   if (masked) {
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (32 * hf + 8 * (r / 4) + r % 4 > lim) sacc[hf][r] = -INFINITY;
+    for (int r = 0; r < 16; ++r)
+      if (8 * (r / 4) + r % 4 > lim) e[r] = -INFINITY;
   }
-  float tmax = -INFINITY;
+  float top = -INFINITY;
 #pragma unroll
-  for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[hf][r]);
+  for (int r = 0; r < 16; ++r) top = fmaxf(top, e[r]);
   // The reference moves only when some row's exponents grew beyond 8: until then probabilities may exceed 1 (by at most
   // 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
-  if (__any(tmax > (m_run == -INFINITY ? -INFINITY : 8.f))) {
-    tmax = max_pair(tmax);
+  if (__any(top > (m_run == -INFINITY ? -INFINITY : 8.f))) {
+    top = max_pair(top);
     const bool first = m_run == -INFINITY;
-    const float d = first ? (tmax == -INFINITY ? 0.f : tmax) : fmaxf(tmax, 0.f);
+    const float d = first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
     const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-d);  // nothing, or NaN, to rescale before the first
-    if (!first || tmax != -INFINITY) m_run = first ? d : m_run + d;
+    if (!first || top != -INFINITY) m_run = first ? d : m_run + d;
     const float ref = m_run == -INFINITY ? 0.f : -m_run;
     lacc[0] *= alpha;
     lacc[1] *= alpha;
-#pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[hf][r] -= d;
+    e -= d;
 #pragma unroll
     for (int r = 0; r < 16; ++r) start[r] = ref;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+    for (int db = 0; db < 4; ++db) oacc[db] *= alpha;
   }
   // probabilities, a pair at a time, beside the products
-  auto soft2 = [&](int g, int j) {
-#pragma unroll
-    for (int e = 2 * j; e < 2 * j + 2; ++e) sacc[g >> 1][8 * (g & 1) + e] = __builtin_amdgcn_exp2f(sacc[g >> 1][8 * (g & 1) + e]);
-  };
-  u32x4 pbuf[2][PARTS];
-  auto cvt2 = [&](int g, int j) {
-    const float a = sacc[g >> 1][8 * (g & 1) + 2 * j], b = sacc[g >> 1][8 * (g & 1) + 2 * j + 1];
-    if constexpr (PARTS == 1) {
-      const bf16x2 pr = {(__bf16)a, (__bf16)b};
-      pbuf[g & 1][0][j] = __builtin_bit_cast(uint32_t, pr);
-    } else {  // the leading part is cut, not rounded
-      const uint32_t wa = __float_as_uint(a), wb = __float_as_uint(b);
-      const bf16x2 rest = {(__bf16)(a - __uint_as_float(wa & 0xFFFF0000u)), (__bf16)(b - __uint_as_float(wb & 0xFFFF0000u))};
-      pbuf[g & 1][0][j] = __builtin_amdgcn_perm(wb, wa, 0x07060302u);
-      pbuf[g & 1][1][j] = __builtin_bit_cast(uint32_t, rest);
+  u32x4 pb[2][PARTS];
+  auto pair = [&](int n) {
+    f32x2 x = {__builtin_amdgcn_exp2f(e[2 * n]), __builtin_amdgcn_exp2f(e[2 * n + 1])};
+    if constexpr (PARTS == 2) {
+      const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]);
+      pb[n >> 2][0][n & 3] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      x[0] -= __uint_as_float(a & 0xFFFF0000u);
+      x[1] -= __uint_as_float(b & 0xFFFF0000u);
     }
+    pb[n >> 2][PARTS - 1][n & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
   };
   // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
   // 4x4x4 products with ones do it on the matrix pipe.
   const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
   s16x4 vlo[4], vhi[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) soft2(0, j);
-#pragma unroll
   for (int i = 0; i < 4; ++i) {
     vlo[i] = SA_VTR(Vt, i & 3, 0);
     vhi[i] = SA_VTR(Vt, i & 3, 8);
   }
 #pragma unroll
-  for (int j = 0; j < 3; ++j) cvt2(0, j);
+  for (int n = 0; n < 4; ++n) pair(n);
   __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-  for (int i = 0; i < 8 * HF; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const int g = i >> 2, db = i & 3;
-    if (db == 0) {
-      cvt2(g, 3);
-#pragma unroll
-      for (int x = 0; x < PARTS; ++x) asm("" : "+v"(pbuf[g & 1][x]));
-    }
-    const s16x8 av = __builtin_shufflevector(vlo[i & 3], vhi[i & 3], 0, 1, 2, 3, 4, 5, 6, 7);
+    const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vlo[db], vhi[db], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
     for (int x = 0; x < PARTS; ++x) {
-      const bf16x8 pb = __builtin_bit_cast(bf16x8, pbuf[g & 1][x]);
-      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), pb, oacc[db], 0, 0, 0);
-      const s16x8 ps = __builtin_bit_cast(s16x8, pb);
+      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g][x]), oacc[db], 0, 0, 0);
+      const s16x8 ps = __builtin_bit_cast(s16x8, pb[g][x]);
       if (db == 0)
         lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
       if (db == 3)
         lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
     }
-    if (i + 4 < 8 * HF) {
-      vlo[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2));
-      vhi[i & 3] = SA_VTR(Vt, (i + 4) & 3, 16 * ((i + 4) >> 2) + 8);
-    }
-    if (g + 1 < 2 * HF) {
-      soft2(g + 1, db);
-      if (db > 0) cvt2(g + 1, db - 1);
+    if (i < 4) {
+      vlo[db] = SA_VTR(Vt, db, 16);
+      vhi[db] = SA_VTR(Vt, db, 24);
+      pair(i + 4);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -267,21 +242,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   const int row = min(r0 + q, p.rows - 1), tok = divided(row, p.by_g), head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const size_t first = (size_t)kvh * p.capacity;
-  const uint8_t *__restrict__ Kh = p.K + first * kRow4 + 32 * gg, *__restrict__ Vh = p.V + first * kRow4 + 16 * (lane & 3);
+  const uint8_t *__restrict__ Kh = p.K + first * kRow4, *__restrict__ Vh = p.V + first * kRow4;
   const uint32_t *__restrict__ ksh = p.k_scale + first, *__restrict__ vsh = p.v_scale + first;
 
   uint4 kc[2], vc[2];  // a lane's two groups of K; pieces of V: rows lane / 4 and 16 further, a group each
   uint32_t ks, vs[2];
-  auto fetch = [&](int t) {  // behind the tokens the last one again: nobody sees it there
-    const size_t kr = min(t * KT + q, p.tokens - 1);
-    kc[0] = *(const uint4 *)(Kh + kr * kRow4);
-    kc[1] = *(const uint4 *)(Kh + kr * kRow4 + 16);
-    ks = ksh[kr];
+  unsigned k_row = q, v_row[2] = {(unsigned)lane >> 2, ((unsigned)lane >> 2) + 16};  // of a tile
+  auto fetch = [&](int t) {
+    if ((t + 1) * KT > p.tokens) {  // the last tile; behind the tokens the last one again: nobody sees it there
+      const unsigned last = (unsigned)(p.tokens - 1 - t * KT);
+      k_row = min(k_row, last);
+      v_row[0] = min(v_row[0], last);
+      v_row[1] = min(v_row[1], last);
+    }
+    const uint8_t *k = Kh + (size_t)t * KT * kRow4, *v = Vh + (size_t)t * KT * kRow4;
+    const char *kscale = (const char *)(ksh + (size_t)t * KT), *vscale = (const char *)(vsh + (size_t)t * KT);
+    kc[0] = *(const uint4 *)(k + (k_row * kRow4 + 32 * gg));
+    kc[1] = *(const uint4 *)(k + (k_row * kRow4 + 32 * gg + 16));
+    ks = *(const uint32_t *)(kscale + 4 * k_row);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const size_t vr = min(t * KT + (lane >> 2) + 16 * i, p.tokens - 1);
-      vc[i] = *(const uint4 *)(Vh + vr * kRow4);
-      vs[i] = vsh[vr];
+      vc[i] = *(const uint4 *)(v + (v_row[i] * kRow4 + 16 * (lane & 3)));
+      vs[i] = *(const uint32_t *)(vscale + 4 * v_row[i]);
     }
   };
   int t = t_begin + wave;
@@ -325,27 +307,26 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
         if (bad) { vc[i] = make_uint4(0u, 0u, 0u, 0u); vs[i] = 0x7F7F7F7Fu; }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float s = scale4(vs[i] >> (8 * (lane & 3)) & 0xFFu);
-      const uint32_t w[4] = {vc[i].x, vc[i].y, vc[i].z, vc[i].w};
-      const int r = (lane >> 2) + 16 * i;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        *(uint4 *)((char *)lds.v[wave] + r * 256 + (((4 * (lane & 3) + k) ^ ((r & 3) * 5)) << 4)) = decode4_8(w[k], s);
-    }
+    const float vscale[2] = {scale4(vs[0] >> (8 * (lane & 3)) & 0xFFu), scale4(vs[1] >> (8 * (lane & 3)) & 0xFFu)};
+    auto put_v = [&](int k) {  // 8 elements of a lane's 64, as bf16 into LDS
+      const uint4 &x = vc[k >> 2];
+      const uint32_t w = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
+      const int r = (lane >> 2) + 16 * (k >> 2);
+      *(uint4 *)((char *)lds.v[wave] + r * 256 + (((4 * (lane & 3) + (k & 3)) ^ ((r & 3) * 5)) << 4)) = decode4_8(w, vscale[k >> 2]);
+    };
     const uint32_t ksw = ks >> (16 * gg);
     asm("" : "+v"(start));  // kept, not made anew
-    f32x16 sacc[1];  // S^T = K Q^T
-    sacc[0] = score_product<0, 0>(kc[0], qc[0], start, ksw, qs[0]);
-    sacc[0] = score_product<0, 1>(kc[0], qc[0], sacc[0], ksw, qs[0]);
-    sacc[0] = score_product<0, 2>(kc[0], qc[0], sacc[0], ksw, qs[0]);
-    sacc[0] = score_product<1, 0>(kc[1], qc[1], sacc[0], ksw, qs[1]);
-    sacc[0] = score_product<1, 1>(kc[1], qc[1], sacc[0], ksw, qs[1]);
-    sacc[0] = score_product<1, 2>(kc[1], qc[1], sacc[0], ksw, qs[1]);
+    f32x16 e;               // S^T = K Q^T, beside it V on its way into LDS
+#define SA_STEP(S, I, FROM) \
+    e = score_product<S, I>(kc[S], qc[S], FROM, ksw, qs[S]); \
+    put_v(4 * S + I); \
+    if (I == 0) put_v(4 * S + 3); \
+    __builtin_amdgcn_sched_barrier(0);
+    SA_STEP(0, 0, start) SA_STEP(0, 1, e) SA_STEP(0, 2, e) SA_STEP(1, 0, e) SA_STEP(1, 1, e) SA_STEP(1, 2, e)
+#undef SA_STEP
     if (t + WK < t_end) fetch(t + WK);
     wave_lds_sync();
-    absorb_exponents<PARTS>(sacc, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, m_run, start, lacc, oacc);
+    absorb_exponents<PARTS>(e, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, m_run, start, lacc, oacc);
     wave_lds_sync();
   }
   if (t_end > t_masked) {
@@ -387,19 +368,29 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
   const int row = min(r0 + q, p.rows - 1), tok = divided(row, p.by_g), head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
 
   const size_t first = (size_t)kvh * p.capacity;
-  const uint8_t *__restrict__ Kh = p.K + first * kRow4 + 16 * b, *__restrict__ Vh = p.V + first * kRow4 + 16 * (lane & 3);
+  const uint8_t *__restrict__ Kh = p.K + first * kRow4, *__restrict__ Vh = p.V + first * kRow4;
   const uint32_t *__restrict__ ksh = p.k_scale + first, *__restrict__ vsh = p.v_scale + first;
 
   uint4 kc[2], vc[2];  // a group of the keys q and q + 16; pieces of V: rows lane / 4 and 16 further, a group each
   uint32_t ks[2], vs[2];
-  auto fetch = [&](int t) {  // behind the tokens the last one again: nobody sees it there
+  unsigned k_row[2] = {(unsigned)q, (unsigned)q + 16}, v_row[2] = {(unsigned)lane >> 2, ((unsigned)lane >> 2) + 16};  // of a tile
+  auto fetch = [&](int t) {
+    if ((t + 1) * KT > p.tokens) {  // the last tile; behind the tokens the last one again: nobody sees it there
+      const unsigned last = (unsigned)(p.tokens - 1 - t * KT);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        k_row[i] = min(k_row[i], last);
+        v_row[i] = min(v_row[i], last);
+      }
+    }
+    const uint8_t *k = Kh + (size_t)t * KT * kRow4, *v = Vh + (size_t)t * KT * kRow4;
+    const char *kscale = (const char *)(ksh + (size_t)t * KT), *vscale = (const char *)(vsh + (size_t)t * KT);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const size_t kr = min(t * KT + q + 16 * i, p.tokens - 1), vr = min(t * KT + (lane >> 2) + 16 * i, p.tokens - 1);
-      kc[i] = *(const uint4 *)(Kh + kr * kRow4);
-      vc[i] = *(const uint4 *)(Vh + vr * kRow4);
-      ks[i] = ksh[kr];
-      vs[i] = vsh[vr];
+      kc[i] = *(const uint4 *)(k + (k_row[i] * kRow4 + 16 * b));
+      vc[i] = *(const uint4 *)(v + (v_row[i] * kRow4 + 16 * (lane & 3)));
+      ks[i] = *(const uint32_t *)(kscale + 4 * k_row[i]);
+      vs[i] = *(const uint32_t *)(vscale + 4 * v_row[i]);
     }
   };
   int t = t_begin + wave;
@@ -481,9 +472,9 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
         l_run += x;
         l_run += y;
         const uint32_t wx = __float_as_uint(x), wy = __float_as_uint(y);
-        const bf16x2 left = {(__bf16)(x - __uint_as_float(wx & 0xFFFF0000u)), (__bf16)(y - __uint_as_float(wy & 0xFFFF0000u))};
+        const f32x2 left = {x - __uint_as_float(wx & 0xFFFF0000u), y - __uint_as_float(wy & 0xFFFF0000u)};
         lead[2 * i + r / 2] = __builtin_amdgcn_perm(wy, wx, 0x07060302u);
-        rest[2 * i + r / 2] = __builtin_bit_cast(uint32_t, left);
+        rest[2 * i + r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, bf16x2));
       }
 #pragma unroll
     for (int db = 0; db < 8; ++db) {
@@ -612,6 +603,7 @@ __device__ inline float largest(const f32x16 (&e)[2]) {
   }
   return max_pair(fmaxf(top[0], top[1]));
 }
+
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p) {
   constexpr int KT = 64, ROWS = kRowsMany;
   constexpr int kMasked = 3;  // tiles that some rows see and others do not, at most: 127 keys
