@@ -105,44 +105,24 @@ __device__ inline f32x16 score_product(const uint4 k, const i32x6 (&q)[kCodes], 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 4, 2, A_BYTE, (int)k_scale, PART, (int)q_scale);
 }
 
-// A tile's exponents (lane = row, accumulator r <-> key 8(r/4) + 4gg + r%4 of 32) into a row's running softmax and its outputs.
-// They are relative to the row's reference m_run, or to 0 before it has one; start: what the next products begin with.
-// masked: keys from place lim + 1 (less 4gg) on are not seen.
-// PARTS: the matrix instruction takes probabilities in bf16.  1: rounded to it, 2^-8 of each; 2: a leading part, cut, and the rest, 2^-15, by twice
-// the products.  launch_cache4_attend says which.
-template <int PARTS>
-__device__ inline void absorb_exponents(f32x16 &e, bool masked, int lim, const uint16_t *Vt, unsigned vbase,
-                                        float &m_run, f32x16 &start, f32x4 (&lacc)[2], f32x16 (&oacc)[4]) {
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  if (masked) {
+// What a lane has of its row (lane & 31 of the wave's).
+struct RowSet {
+  i32x6 qc[2][kCodes];
+  uint32_t qs[2];
+  float m, l;         // the reference of its exponents, the sum of its probabilities
+  int row, see, all;  // the row; the last key that it sees; the last that every row of the wave sees
+};
+
+template <int N>
+struct Int { static constexpr int value = N; };
+
+// Probabilities of pairs N .. N + COUNT - 1 (a pair: accumulators 2N, 2N + 1) as the products take them, in bf16.  PARTS 1: rounded to it, 2^-8 of
+// each; 2: a leading part, cut, and the rest, 2^-15, by twice the products.  launch_cache4_attend says which.
+template <int N, int COUNT, int HF, int PARTS>
+__device__ inline void probabilities(f32x16 (&e)[HF], u32x4 (&pb)[2 * HF][PARTS]) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (8 * (r / 4) + r % 4 > lim) e[r] = -INFINITY;
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) top = fmaxf(top, e[r]);
-  // The reference moves only when some row's exponents grew beyond 8: until then probabilities may exceed 1 (by at most
-  // 256x), which fp32 sums and bf16 P hold easily, and the 64 accumulators are not rescaled.
-  if (__any(top > (m_run == -INFINITY ? -INFINITY : 8.f))) {
-    top = max_pair(top);
-    const bool first = m_run == -INFINITY;
-    const float d = first ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
-    const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-d);  // nothing, or NaN, to rescale before the first
-    if (!first || top != -INFINITY) m_run = first ? d : m_run + d;
-    const float ref = m_run == -INFINITY ? 0.f : -m_run;
-    lacc[0] *= alpha;
-    lacc[1] *= alpha;
-    e -= d;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) start[r] = ref;
-#pragma unroll
-    for (int db = 0; db < 4; ++db) oacc[db] *= alpha;
-  }
-  // probabilities, a pair at a time, beside the products
-  u32x4 pb[2][PARTS];
-  auto pair = [&](int n) {
-    f32x2 x = {__builtin_amdgcn_exp2f(e[2 * n]), __builtin_amdgcn_exp2f(e[2 * n + 1])};
+  for (int n = N; n < N + COUNT; ++n) {
+    f32x2 x = {__builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7)]), __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7) + 1])};
     if constexpr (PARTS == 2) {
       const uint32_t a = __float_as_uint(x[0]), b = __float_as_uint(x[1]);
       pb[n >> 2][0][n & 3] = __builtin_amdgcn_perm(b, a, 0x07060302u);
@@ -150,42 +130,45 @@ __device__ inline void absorb_exponents(f32x16 &e, bool masked, int lim, const u
       x[1] -= __uint_as_float(b & 0xFFFF0000u);
     }
     pb[n >> 2][PARTS - 1][n & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-  };
-  // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
-  // 4x4x4 products with ones do it on the matrix pipe.
-  const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
-  s16x4 vlo[4], vhi[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    vlo[i] = SA_VTR(Vt, i & 3, 0);
-    vhi[i] = SA_VTR(Vt, i & 3, 8);
   }
-#pragma unroll
-  for (int n = 0; n < 4; ++n) pair(n);
-  __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int g = i >> 2, db = i & 3;
-    const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vlo[db], vhi[db], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-    for (int x = 0; x < PARTS; ++x) {
-      oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g][x]), oacc[db], 0, 0, 0);
-      const s16x8 ps = __builtin_bit_cast(s16x8, pb[g][x]);
-      if (db == 0)
-        lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
-      if (db == 3)
-        lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
-    }
-    if (i < 4) {
-      vlo[db] = SA_VTR(Vt, db, 16);
-      vhi[db] = SA_VTR(Vt, db, 24);
-      pair(i + 4);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  __builtin_amdgcn_s_setprio(0);
 }
 
+// Keys that a row does not see, from place lim + 1 (less 4gg) of the tile on.
+template <int HF>
+__device__ inline void hide(f32x16 (&e)[HF], int lim) {
+#pragma unroll
+  for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (32 * hf + 8 * (k / 4) + k % 4 > lim) e[hf][k] = -INFINITY;
+}
+// The largest of a row's exponents of a tile.
+template <int HF>
+__device__ inline float largest(const f32x16 (&e)[HF]) {
+  float top[HF];
+#pragma unroll
+  for (int hf = 0; hf < HF; ++hf) {
+    top[hf] = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) top[hf] = fmaxf(top[hf], e[hf][k]);
+  }
+  return max_pair(HF == 1 ? top[0] : fmaxf(top[0], top[HF - 1]));
+}
+
+// With 32 and 128 rows a workgroup probabilities are 2^exponent as it is: fp32 and bf16 hold them from 2^-126 to 2^127, so that nothing has to be
+// searched, subtracted or rescaled on the way.  V is multiplied by 2^40, so that small values times small probabilities are normal
+// numbers: the least of both, 2^-101 and 2^-40, make 2^-101.  (The sum is, too, so that it is as if -40 had been subtracted.)  Where that is not
+// enough (a row's sum beyond 2^80 or below 2^-40, or an output that is no number, of V beyond 2^85 or NaN) the rows are done once more, with
+// their largest exponents subtracted and V as it is.
+constexpr float kUp = 0x1p40f, kUpRef = -40.f;
+__device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
+  float odd[4] = {};  // 0, or NaN where an output is no number
+#pragma unroll
+  for (int k = 0; k < 16; ++k)
+#pragma unroll
+    for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
+  return l > 0x1p-40f && l < 0x1p80f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f;
+}
 // The groups of V that are NaN among the keys first .. first + 63 (rowbad: a byte for each, a bit for each group; 0 from key `end` on), for a row
 // that sees keys up to `see`.
 __device__ inline void put_nan(const uint8_t *rowbad, int first, int end, int see, f32x16 (&o)[4]) {
@@ -238,8 +221,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   const int per = divided(n_tiles + p.S - 1, p.by_S);
   const int t_begin = min(sp * per, n_tiles), t_end = min(t_begin + per, n_tiles);
 
-  // this lane's row, and the last key that it sees
-  const int row = min(r0 + q, p.rows - 1), tok = divided(row, p.by_g), head = kvh * p.g + (row - tok * p.g), see = p.pos + tok;
+  RowSet r;
+  r.row = min(r0 + q, p.rows - 1);
+  const int tok = divided(r.row, p.by_g), head = kvh * p.g + (r.row - tok * p.g);
+  r.see = p.pos + tok;
 
   const size_t first = (size_t)kvh * p.capacity;
   const uint8_t *__restrict__ Kh = p.K + first * kRow4, *__restrict__ Vh = p.V + first * kRow4;
@@ -266,78 +251,133 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
       vs[i] = *(const uint32_t *)(vscale + 4 * v_row[i]);
     }
   };
-  int t = t_begin + wave;
-  if (t < t_end) fetch(t);
+  const int t_first = t_begin + wave;
+  if (t_first < t_end) fetch(t_first);
 
   // Q: the groups 2gg and 2gg + 1 of a row, as the lane's K
-  i32x6 qc[2][kCodes];
-  uint32_t qs[2];
   const uint16_t *qrow = p.Q + (size_t)head * p.q_hs + (size_t)tok * p.q_rs + 64 * gg;
 #pragma unroll 1
   for (int s = 0; s < 2; ++s) {  // one after the other, in half the code
 #pragma unroll
-    for (int i = 0; i < kCodes; ++i) qc[0][i] = qc[1][i];
-    qs[0] = qs[1];
-    qs[1] = cut_query(qrow + 32 * s, p.c, qc[1]);
+    for (int i = 0; i < kCodes; ++i) r.qc[0][i] = r.qc[1][i];
+    r.qs[0] = r.qs[1];
+    r.qs[1] = cut_query(qrow + 32 * s, p.c, r.qc[1]);
   }
-
-  f32x16 oacc[4];
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-  float m_run = -INFINITY;
-  f32x16 start = {};  // minus the reference, 0 before there is one
-  f32x4 lacc[2] = {};
 
   unsigned vbase;
   {
-    const int r = lane & 15, part = (lane >> 4) & 1, vrow = 4 * gg + (r >> 2);
-    vbase = (unsigned)(vrow * 256) | (unsigned)(((2 * part + ((r & 3) >> 1)) ^ ((vrow & 3) * 5)) << 4) | (unsigned)((r & 1) << 3);
+    const int x = lane & 15, part = (lane >> 4) & 1, vrow = 4 * gg + (x >> 2);
+    vbase = (unsigned)(vrow * 256) | (unsigned)(((2 * part + ((x & 3) >> 1)) ^ ((vrow & 3) * 5)) << 4) | (unsigned)((x & 1) << 3);
   }
-  for (; t < t_end; t += WK) {
-    // A row that does not see a key gives it weight 0, and 0 x NaN is not 0: in tiles that only some rows see, groups of V
-    // that are NaN stay out of the products and come back at the end for the rows that do see them.
-    if (t >= t_masked) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  f32x16 oacc[4];
+  f32x4 lacc[2];
+  auto run = [&](auto AGAIN) {
+    constexpr bool kAgain = decltype(AGAIN)::value != 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bool bad = (vs[i] >> (8 * (lane & 3)) & 0xFFu) == kNanScale;
-        const uint64_t who = __ballot(bad);
-        if ((lane & 3) == 0) rowbad[(t - t_masked) * KT + (lane >> 2) + 16 * i] = (uint8_t)(who >> lane & 15ull);
-        if (bad) { vc[i] = make_uint4(0u, 0u, 0u, 0u); vs[i] = 0x7F7F7F7Fu; }
+    for (int db = 0; db < 4; ++db) oacc[db] = f32x16{};
+    lacc[0] = lacc[1] = f32x4{};
+    for (int t = t_first; t < t_end; t += WK) {
+      // A row that does not see a key gives it weight 0, and 0 x NaN is not 0: in tiles that only some rows see, groups of V
+      // that are NaN stay out of the products and come back at the end for the rows that do see them.
+      if (t >= t_masked) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool bad = (vs[i] >> (8 * (lane & 3)) & 0xFFu) == kNanScale;
+          const uint64_t who = __ballot(bad);
+          if ((lane & 3) == 0) rowbad[(t - t_masked) * KT + (lane >> 2) + 16 * i] = (uint8_t)(who >> lane & 15ull);
+          if (bad) { vc[i] = make_uint4(0u, 0u, 0u, 0u); vs[i] = 0x7F7F7F7Fu; }
+        }
       }
-    }
-    const float vscale[2] = {scale4(vs[0] >> (8 * (lane & 3)) & 0xFFu), scale4(vs[1] >> (8 * (lane & 3)) & 0xFFu)};
-    auto put_v = [&](int k) {  // 8 elements of a lane's 64, as bf16 into LDS
-      const uint4 &x = vc[k >> 2];
-      const uint32_t w = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
-      const int r = (lane >> 2) + 16 * (k >> 2);
-      *(uint4 *)((char *)lds.v[wave] + r * 256 + (((4 * (lane & 3) + (k & 3)) ^ ((r & 3) * 5)) << 4)) = decode4_8(w, vscale[k >> 2]);
-    };
-    const uint32_t ksw = ks >> (16 * gg);
-    asm("" : "+v"(start));  // kept, not made anew
-    f32x16 e;               // S^T = K Q^T, beside it V on its way into LDS
-#define SA_STEP(S, I, FROM) \
-    e = score_product<S, I>(kc[S], qc[S], FROM, ksw, qs[S]); \
-    put_v(4 * S + I); \
-    if (I == 0) put_v(4 * S + 3); \
-    __builtin_amdgcn_sched_barrier(0);
-    SA_STEP(0, 0, start) SA_STEP(0, 1, e) SA_STEP(0, 2, e) SA_STEP(1, 0, e) SA_STEP(1, 1, e) SA_STEP(1, 2, e)
+      constexpr float up = kAgain ? 1.f : kUp;
+      const float vscale[2] = {scale4(vs[0] >> (8 * (lane & 3)) & 0xFFu) * up, scale4(vs[1] >> (8 * (lane & 3)) & 0xFFu) * up};
+      auto put_v = [&](int k) {  // 8 elements of a lane's 64, as bf16 into LDS
+        const uint4 &x = vc[k >> 2];
+        const uint32_t w = (k & 3) == 0 ? x.x : (k & 3) == 1 ? x.y : (k & 3) == 2 ? x.z : x.w;
+        const int at = (lane >> 2) + 16 * (k >> 2);
+        *(uint4 *)((char *)lds.v[wave] + at * 256 + (((4 * (lane & 3) + (k & 3)) ^ ((at & 3) * 5)) << 4)) = decode4_8(w, vscale[k >> 2]);
+      };
+      const uint32_t ksw = ks >> (16 * gg);
+      f32x16 e[1];  // S^T = K Q^T (lane = row, accumulator r <-> key 8(r/4) + 4gg + r%4), beside it V on its way into LDS
+#define SA_STEP(S, I) \
+      e[0] = score_product<S, I>(kc[S], r.qc[S], S == 0 && I == 0 ? f32x16{} : e[0], ksw, r.qs[S]); \
+      put_v(4 * S + I); \
+      if (I == 0) put_v(4 * S + 3); \
+      __builtin_amdgcn_sched_barrier(0);
+      SA_STEP(0, 0) SA_STEP(0, 1) SA_STEP(0, 2) SA_STEP(1, 0) SA_STEP(1, 1) SA_STEP(1, 2)
 #undef SA_STEP
-    if (t + WK < t_end) fetch(t + WK);
-    wave_lds_sync();
-    absorb_exponents<PARTS>(e, (t + 1) * KT - 1 > seen_all, see - t * KT - 4 * gg, lds.v[wave], vbase, m_run, start, lacc, oacc);
-    wave_lds_sync();
+      if (t + WK < t_end) fetch(t + WK);
+      if (kAgain) e[0] -= r.m;
+      if ((t + 1) * KT - 1 > seen_all) hide(e, r.see - t * KT - 4 * gg);
+      wave_lds_sync();
+      u32x4 pb[2][PARTS];
+      s16x4 vlo[4], vhi[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        vlo[i] = SA_VTR(lds.v[wave], i & 3, 0);
+        vhi[i] = SA_VTR(lds.v[wave], i & 3, 8);
+      }
+      probabilities<0, 4>(e, pb);
+      __builtin_amdgcn_s_setprio(1);
+      // The normaliser sums the probabilities as multiplied, so that a row stays a convex combination of its V rows;
+      // 4x4x4 products with ones do it on the matrix pipe.
+      const s16x4 ones4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+      auto step = [&](auto I) {
+        constexpr int i = decltype(I)::value, g = i >> 2, db = i & 3;
+        const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vlo[db], vhi[db], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) {
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g][x]), oacc[db], 0, 0, 0);
+          const s16x8 ps = __builtin_bit_cast(s16x8, pb[g][x]);
+          if constexpr (db == 0) lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
+          if constexpr (db == 3) lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
+        }
+        if constexpr (i < 4) {
+          vlo[db] = SA_VTR(lds.v[wave], db, 16);
+          vhi[db] = SA_VTR(lds.v[wave], db, 24);
+          probabilities<i + 4, 1>(e, pb);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      step(Int<0>()); step(Int<1>()); step(Int<2>()); step(Int<3>()); step(Int<4>()); step(Int<5>()); step(Int<6>()); step(Int<7>());
+      __builtin_amdgcn_s_setprio(0);
+      wave_lds_sync();
+    }
+    r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
+  };
+  run(Int<0>());
+  const bool sees = t_first < t_end && r.see >= t_first * KT;
+  const bool again = __any(sees && !in_range(r.l, oacc));
+  r.m = sees ? kUpRef : -INFINITY;
+  r.l *= kUp;
+  if (again) {  // this wave's keys
+    float top = -INFINITY;
+    for (int t = t_first; t < t_end; t += WK) {
+      fetch(t);
+      const uint32_t ksw = ks >> (16 * gg);
+      f32x16 e[1] = {};
+#define SA_STEP(S, I) e[0] = score_product<S, I>(kc[S], r.qc[S], e[0], ksw, r.qs[S]);
+      SA_STEP(0, 0) SA_STEP(0, 1) SA_STEP(0, 2) SA_STEP(1, 0) SA_STEP(1, 1) SA_STEP(1, 2)
+#undef SA_STEP
+      hide(e, r.see - t * KT - 4 * gg);
+      top = fmaxf(top, largest(e));
+    }
+    r.m = top == -INFINITY ? 0.f : top;
+    k_row = q;  // the walk's last tile changed them
+    v_row[0] = (unsigned)lane >> 2;
+    v_row[1] = ((unsigned)lane >> 2) + 16;
+    fetch(t_first);
+    run(Int<1>());
+    r.m = top;
   }
   if (t_end > t_masked) {
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) {
       if ((t - t_begin) % WK != wave) continue;  // another wave's tile
-      put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, see, oacc);
+      put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
     }
   }
-  const float l_run = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
-  put_waves(p, kvh, r0, sp, m_run, l_run, oacc, &lds.o[0][0][0], s_m, s_l);
+  put_waves(p, kvh, r0, sp, r.m, r.l, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
 // Steps: 16 query rows a workgroup, every wave its own keys, tiles of 32 of them.  One v_mfma_scale_f32_16x16x128 takes 16 keys, whole rows of K: a
@@ -547,14 +587,6 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
 
 // Many rows: four waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
 // in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.
-// What a lane has of its row (lane & 31 of the wave's).
-struct RowSet {
-  i32x6 qc[2][kCodes];
-  uint32_t qs[2];
-  float m, l;         // the reference of its exponents, the sum of its probabilities
-  int row, see, all;  // the row; the last key that it sees; the last that every row of the wave sees
-};
-
 // K Q^T of half a tile (the codes of d-slab S) for both halves of the keys, product I of kCodes.
 template <int S, int I>
 __device__ inline void score_pair(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (&e)[2], const uint32_t (&ks)[2]) {
@@ -570,38 +602,6 @@ __device__ inline void scores(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (
   score_pair<1, 0>(kf, r, e, ks);
   score_pair<1, 1>(kf, r, e, ks);
   score_pair<1, 2>(kf, r, e, ks);
-}
-
-template <int N>
-struct Int { static constexpr int value = N; };
-
-// Probabilities of pairs N .. N + COUNT - 1 of 16 (a pair: accumulators 2N, 2N + 1), rounded to bf16, as the products take them.
-template <int N, int COUNT>
-__device__ inline void probabilities(f32x16 (&e)[2], u32x4 (&pb)[4]) {
-#pragma unroll
-  for (int n = N; n < N + COUNT; ++n) {
-    const f32x2 x = {__builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7)]), __builtin_amdgcn_exp2f(e[n >> 3][2 * (n & 7) + 1])};
-    pb[n >> 2][n & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-  }
-}
-
-// Keys that a row does not see, from place lim + 1 (less 4gg) of the tile on.
-__device__ inline void hide(f32x16 (&e)[2], int lim) {
-#pragma unroll
-  for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-      if (32 * hf + 8 * (k / 4) + k % 4 > lim) e[hf][k] = -INFINITY;
-}
-// The largest of a row's exponents of a tile.
-__device__ inline float largest(const f32x16 (&e)[2]) {
-  float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    top[0] = fmaxf(top[0], e[0][k]);
-    top[1] = fmaxf(top[1], e[1][k]);
-  }
-  return max_pair(fmaxf(top[0], top[1]));
 }
 
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p) {
@@ -715,20 +715,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
   const bool idle = r0 + 32 * wave >= p.rows;  // a wave without rows only turns its part of V into bf16
   f32x16 oacc[4];
   f32x4 lacc[2];
-  // Probabilities are 2^e as it is: fp32 and bf16 hold them from 2^-126 to 2^127, so that nothing has to be searched, subtracted or rescaled.  Where
-  // that was too little (a row's sum beyond 2^100, or below 2^-20, where small values of V times small probabilities would leave fp32, or an
-  // output that is no number) the workgroup looks for the rows' largest exponents
-  // and starts anew, with them subtracted.
-  r.m = 0.f;
   auto run = [&](auto AGAIN) {
     constexpr bool kAgain = decltype(AGAIN)::value != 0;
+    constexpr float up = kAgain ? 1.f : kUp;
 #pragma unroll
     for (int db = 0; db < 4; ++db) oacc[db] = f32x16{};
     lacc[0] = lacc[1] = f32x4{};
     if (t_begin < t_end) {
       if (t_begin >= t_masked) screen(t_begin);
       {
-        const float s = scale4(vs >> (8 * vg) & 0xFFu);
+        const float s = scale4(vs >> (8 * vg) & 0xFFu) * up;
 #pragma unroll
         for (int k = 0; k < 4; ++k) put_v(0, k, s);
       }
@@ -745,7 +741,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
           fetch_ks(t + 1);
           if (t + 1 >= t_masked) screen(t + 1);
         }
-        return scale4(vs >> (8 * vg) & 0xFFu);
+        return scale4(vs >> (8 * vg) & 0xFFu) * up;
       };
       auto fetch_next = [&](int t) {
         if (t >= t_end) return;
@@ -776,7 +772,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
           }
         }
         if (j0 + KT - 1 > r.all) hide(e, r.see - j0 - 4 * gg);
-        u32x4 pb[4];
+        u32x4 pb[4][1];
         s16x4 vlo[4], vhi[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -791,8 +787,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
         auto step = [&](auto I) {
           constexpr int i = decltype(I)::value, g = i >> 2, db = i & 3;
           const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vlo[db], vhi[db], 0, 1, 2, 3, 4, 5, 6, 7));
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g]), oacc[db], 0, 0, 0);
-          const s16x8 ps = __builtin_bit_cast(s16x8, pb[g]);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, __builtin_bit_cast(bf16x8, pb[g][0]), oacc[db], 0, 0, 0);
+          const s16x8 ps = __builtin_bit_cast(s16x8, pb[g][0]);
           if constexpr (db == 0) lacc[0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 0, 1, 2, 3), lacc[0], 0, 0, 0);
           if constexpr (db == 3) lacc[1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(ones4, __builtin_shufflevector(ps, ps, 4, 5, 6, 7), lacc[1], 0, 0, 0);
           if constexpr (i + 4 < 16) {
@@ -824,13 +820,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
   };
   run(Int<0>());
-  float odd[4] = {};  // 0, or NaN where an output is no number
-#pragma unroll
-  for (int k = 0; k < 16; ++k)
-#pragma unroll
-    for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
-  const bool good = idle || r.see < t_begin * KT || (r.l > 0x1p-20f && r.l < 0x1p100f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f);
-  if (__builtin_amdgcn_readfirstlane(__syncthreads_or(!good)) && t_begin < t_end) {
+  const bool sees = t_begin < t_end && r.see >= t_begin * KT;
+  const bool again = __builtin_amdgcn_readfirstlane(__syncthreads_or(!idle && sees && !in_range(r.l, oacc)));
+  r.m = sees ? kUpRef : -INFINITY;
+  r.l *= kUp;
+  if (again) {
     float top = -INFINITY;
     offsets(t_begin < n_whole ? KT : p.tokens - t_begin * KT);
     for (int t = t_begin; t < t_end; ++t) {
@@ -852,13 +846,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     r.m = top == -INFINITY ? 0.f : top;
     begin();
     run(Int<1>());
-    if (top == -INFINITY) r.m = top;
+    r.m = top;
   }
   if (t_end > t_masked) {
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
   }
-  if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.see < t_begin * KT ? -INFINITY : r.m, r.l, oacc);
+  if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.m, r.l, oacc);
 }
 
 // Rows x splits that the scratch holds: two workgroups of 128 rows a compute unit, as for the 8-bit cache.
