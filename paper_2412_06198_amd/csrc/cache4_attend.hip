@@ -859,22 +859,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 256; }
 
 // Which kernel, and into how many splits the keys go: the least of an estimate over the three kernels and over splits that fill a quarter of the card, a
-// half, .. all that a compute unit holds at once.  The terms were fitted (us) to some 6000 measurements of 750 drawn shapes of 4 to 64
-// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 1.0 % slower than the best of all kernels and splits in the
-// mean, and 25 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
-//                                              16 rows   32 rows   128 rows
-//   start and end                              4.1       5.8       5.15
-//   keys of a round of a workgroup's waves     128       128       64
-//   a round, up to a workgroup a compute unit  0.9       0.69      0.95
-//   more of that for each further one          0.3       0.8       0.35
-//   more at the start for each further one     1.3       0.18
-//   workgroups a compute unit at once          4         2         2
+// half, .. all that a compute unit holds at once.  The terms were fitted (us) to some 9000 measurements of 1100 drawn shapes of 4 to 64
+// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 0.9 % slower than the best of all kernels and splits in the
+// mean, and 21 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
+//                                              16 rows   32 rows, up to 64 in all   32 rows   128 rows
+//   start and end                              4.1       5.6                        5.6       5.15
+//   keys of a round of a workgroup's waves     128       128                        128       64
+//   a round, up to a workgroup a compute unit  0.9       0.92                       0.69      0.95
+//   more of that for each further one          0.3       0.8                        0.8       0.35
+//   more at the start for each further one     1.3       0.3                        0.3
+//   workgroups a compute unit at once          4         2                          2         2
 //   more than that: their number times this, of which rows see less than the longest one, and 0.6 of a start
-//   a join: its launch 2.7, and 1 KB written and read for each row and split
+//   a join: its launch 2.5, and 1 KB written and read for each row and split
 struct Plan { int rows, S; };
 Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
   struct Kernel { int rows, keys, waves, most; float start, more_start, round, more_round; };  // keys of a tile, waves that share out the tiles
-  const Kernel kernels[3] = {{kRowsStep, 32, 4, 4, 4.1f, 1.3f, 0.9f, 0.3f}, {kRowsFew, 32, 4, 2, 5.8f, 0.18f, 0.69f, 0.8f}, {kRowsMany, 64, 1, 2, 5.15f, 0.f, 0.95f, 0.35f}};
+  const Kernel kernels[3] = {{kRowsStep, 32, 4, 4, 4.1f, 1.3f, 0.9f, 0.3f}, {kRowsFew, 32, 4, 2, 5.6f, 0.3f, rows <= 2 * kRowsFew ? 0.92f : 0.69f, 0.8f}, {kRowsMany, 64, 1, 2, 5.15f, 0.f, 0.95f, 0.35f}};
   const float mean = 0.5f + 0.5f * pos / tokens;  // keys that a row sees, against all
   const int64_t all = (int64_t)rows * sh.Hkv;
   Plan best = {kRowsStep, 1};
@@ -892,7 +892,7 @@ Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
       const float body = k.more_start * beside + per * (k.round + k.more_round * beside);
       float t = k.start + body;
       if (load > k.most) t = std::max(t, load / k.most * (0.6f * k.start + k.more_start * beside + per * (k.round + k.more_round * beside) * mean));
-      if (S > 1) t += 2.7f + all * S * 0.0003f;
+      if (S > 1) t += 2.5f + all * S * 0.0003f;
       if (t < least) { least = t; best = {k.rows, S}; }
     }
   }
