@@ -859,22 +859,26 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
 size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 256; }
 
 // Which kernel, and into how many splits the keys go: the least of an estimate over the three kernels and over splits that fill a quarter of the card, a
-// half, .. all that a compute unit holds at once.  The terms were fitted (us) to some 9000 measurements of 1100 drawn shapes of 4 to 64
-// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 0.9 % slower than the best of all kernels and splits in the
-// mean, and 21 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
+// half, .. all that a compute unit holds at once.  The terms were fitted (us) to some 13000 measurements of 1500 drawn shapes of 4 to 64
+// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 0.5 % slower than the best of all kernels and splits in the
+// mean, and 22 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
 //                                              16 rows   32 rows, up to 64 in all   32 rows   128 rows
-//   start and end                              4.1       5.6                        5.6       5.15
+//   start and end                              3.45      5.65                       5.65      5.2
 //   keys of a round of a workgroup's waves     128       128                        128       64
-//   a round, up to a workgroup a compute unit  0.9       0.92                       0.69      0.95
-//   more of that for each further one          0.3       0.8                        0.8       0.35
-//   more at the start for each further one     1.3       0.3                        0.3
+//   a round, up to a workgroup a compute unit  0.92      1.0                        0.73      0.95
+//   more of that for each further one          0.28      0.75                       0.8       0.3
+//   more at the start for each further one     1.25      0.37                       0.37
 //   workgroups a compute unit at once          4         2                          2         2
+//   further ones: as many as on average; with 16 and 128 rows halfway from there to the compute units that have the most
 //   more than that: their number times this, of which rows see less than the longest one, and 0.6 of a start
-//   a join: its launch 2.5, and 1 KB written and read for each row and split
+//   a join: its launch 2.7, and 1 KB written and read for each row and split
 struct Plan { int rows, S; };
 Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
-  struct Kernel { int rows, keys, waves, most; float start, more_start, round, more_round; };  // keys of a tile, waves that share out the tiles
-  const Kernel kernels[3] = {{kRowsStep, 32, 4, 4, 4.1f, 1.3f, 0.9f, 0.3f}, {kRowsFew, 32, 4, 2, 5.6f, 0.3f, rows <= 2 * kRowsFew ? 0.92f : 0.69f, 0.8f}, {kRowsMany, 64, 1, 2, 5.15f, 0.f, 0.95f, 0.35f}};
+  struct Kernel { int rows, keys, waves, most; float start, more_start, round, more_round, full; };  // keys of a tile, waves that share out the tiles
+  const bool parts = rows <= 2 * kRowsFew;
+  const Kernel kernels[3] = {{kRowsStep, 32, 4, 4, 3.45f, 1.25f, 0.92f, 0.28f, 0.5f},
+                             {kRowsFew, 32, 4, 2, 5.65f, 0.37f, parts ? 1.f : 0.73f, parts ? 0.75f : 0.8f, 0.f},
+                             {kRowsMany, 64, 1, 2, 5.2f, 0.f, 0.95f, 0.3f, 0.5f}};
   const float mean = 0.5f + 0.5f * pos / tokens;  // keys that a row sees, against all
   const int64_t all = (int64_t)rows * sh.Hkv;
   Plan best = {kRowsStep, 1};
@@ -888,11 +892,12 @@ Plan plan_of(const Shape &sh, int rows, int tokens, int pos) {
       if (quarters > 4 * k.most || (quarters > 0 && fill <= 1)) continue;
       const int S0 = (int)std::max<int64_t>(1, std::min<int64_t>(fill, top));
       const int share = (tiles + S0 - 1) / S0, S = (tiles + share - 1) / share, per = (share + k.waves - 1) / k.waves;
-      const float load = (float)wgs * S / sh.n_cu, beside = std::min(std::max(load - 1.f, 0.f), k.most - 1.f);
+      const float load = (float)wgs * S / sh.n_cu;
+      const float beside = std::min(std::max(load + k.full * (std::ceil(load) - load) - 1.f, 0.f), k.most - 1.f);
       const float body = k.more_start * beside + per * (k.round + k.more_round * beside);
       float t = k.start + body;
       if (load > k.most) t = std::max(t, load / k.most * (0.6f * k.start + k.more_start * beside + per * (k.round + k.more_round * beside) * mean));
-      if (S > 1) t += 2.5f + all * S * 0.0003f;
+      if (S > 1) t += 2.7f + all * S * 0.0003f;
       if (t < least) { least = t; best = {k.rows, S}; }
     }
   }

@@ -13,9 +13,9 @@ pytestmark = pytest.mark.gpu
 
 # heads, tokens, before, (rows of a workgroup, whether in splits)
 FORMS = [((4, 4), 3, 0, (16, False)), ((8, 2), 61, 333, (16, False)), ((4, 4), 700, 5, (16, False)), ((16, 2), 12, 3001, (16, True)), ((128, 2), 5, 3001, (16, True)),
-         ((64, 1), 130, 0, (32, False)), ((64, 8), 191, 640, (32, False)), ((8, 1), 191, 1000, (32, True)), ((6, 2), 100, 3001, (32, True)),
-         ((4, 4), 50, 15000, (32, True)), ((32, 8), 13, 9000, (32, True)), ((40, 1), 47, 4000, (32, True)),
-         ((128, 2), 61, 0, (128, False)), ((128, 2), 130, 5, (128, False)), ((128, 2), 100, 70, (128, False)), ((64, 1), 400, 640, (128, False)),
+         ((64, 1), 130, 0, (32, False)), ((64, 8), 191, 640, (32, False)), ((8, 1), 191, 2000, (32, True)), ((6, 2), 150, 3001, (32, True)),
+         ((8, 8), 50, 9000, (32, True)), ((32, 8), 13, 9000, (32, True)), ((40, 1), 47, 4000, (32, True)),
+         ((128, 2), 160, 0, (128, False)), ((128, 2), 130, 5, (128, False)), ((128, 2), 100, 70, (128, False)), ((64, 1), 400, 640, (128, False)),
          ((128, 2), 333, 1000, (128, False)), ((8, 1), 700, 6000, (128, True)), ((64, 1), 47, 9000, (128, True)), ((4, 4), 400, 20000, (128, True))]
 
 
