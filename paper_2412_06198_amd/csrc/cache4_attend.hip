@@ -159,7 +159,9 @@ __device__ inline float largest(const f32x16 (&e)[HF]) {
 // searched, subtracted or rescaled on the way.  V is multiplied by 2^40, so that small values times small probabilities are normal
 // numbers: the least of both, 2^-101 and 2^-40, make 2^-101.  (The sum is, too, so that it is as if -40 had been subtracted.)  Where that is not
 // enough (a row's sum beyond 2^80 or below 2^-40, or an output that is no number, of V beyond 2^85 or NaN) the rows are done once more, with
-// their largest exponents subtracted and V as it is.
+// their largest exponents subtracted and V as it is.  With 128 rows a long walk looks at its first tile ahead, and where that is far from 0
+// already, subtracts the largest exponents of this tile from the start (2048 tokens of 32 heads at 64K keys, all scores 40 lower: 4000 us without
+// the look, 1580 with it; as they come 1555).
 constexpr float kUp = 0x1p40f, kUpRef = -40.f;
 __device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
   float odd[4] = {};  // 0, or NaN where an output is no number
@@ -197,8 +199,9 @@ __device__ inline float sum_blocks(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads the half row of K
-// that it multiplies itself.
+// 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads the half row of K that it multiplies
+// itself, so that only V goes through LDS, between the products of K.  Bound: one tile after the other, which two waves a SIMD half hide:
+// products, their exponentials, V's way through LDS.  500 tokens of 32 heads at 1000 keys 16.7 us, 50 at 5000 16.4 with the join (8 bits: 19.7 at 500).
 template <int PARTS>
 __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
@@ -382,7 +385,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
 
 // Steps: 16 query rows a workgroup, every wave its own keys, tiles of 32 of them.  One v_mfma_scale_f32_16x16x128 takes 16 keys, whole rows of K: a
 // lane reads one group of a key and multiplies it with the same group of its query row (lane & 15).  Half the products, exponentials and registers of 32
-// rows, so that four waves a SIMD, instead of two, have reads on their way.
+// rows, so that four waves a SIMD, instead of two, have reads on their way.  Bound: HBM on long caches, one token of 32 heads at 128K keys reads 143 MB in
+// 28.0 us (5.1 TB/s), 32.3 with the join (32 rows a workgroup: 39.6); the chain of reads on short ones, 5 tokens of 8 heads on one KV head at 10K keys 9.1.
 __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p) {
   constexpr int KT = 32, WK = kThreads / 64, ROWS = kRowsStep;
   constexpr int kMasked = 2;  // tiles that some rows see and others do not, at most: 15 keys
@@ -585,8 +589,6 @@ __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p
   }
 }
 
-// Many rows: four waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
-// in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.
 // K Q^T of half a tile (the codes of d-slab S) for both halves of the keys, product I of kCodes.
 template <int S, int I>
 __device__ inline void score_pair(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (&e)[2], const uint32_t (&ks)[2]) {
@@ -604,8 +606,13 @@ __device__ inline void scores(const uint4 (&kf)[2][2], const RowSet &r, f32x16 (
   score_pair<1, 2>(kf, r, e, ks);
 }
 
+// Many rows: four waves of 32 query rows each, which share tiles of 64 keys.  K goes from memory into LDS as it is (the LDS DMA, no registers), V
+// in bf16, from registers that were read a tile ahead; beside the products of a tile, V of the next one.  Bound: the matrix pipe at the power
+// limit, 2048 tokens of 32 heads at 64K keys 1505 to 1560 us by card, 1.44 to 1.39 PFLOP/s (8 bits: 1650 to 1790; a library product of bf16 1.35), with
+// the clock at 2.0 GHz.  64 rows a wave, eight waves that share V or the keys of a tile, and a tile's products begun beside the last one's end were slower.
 __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p) {
   constexpr int KT = 64, ROWS = kRowsMany;
+  constexpr int kLong = 256;  // tiles of a walk that is worth a look ahead
   constexpr int kMasked = 3;  // tiles that some rows see and others do not, at most: 127 keys
   __shared__ __attribute__((aligned(16))) uint8_t Ks[2][KT * kRow4];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[2][KT * 128];
@@ -819,20 +826,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     }
     r.l = sum_pair(lacc[0][0] + lacc[1][0]);  // the keys of both lanes of a row
   };
-  run(Int<0>());
-  const bool sees = t_begin < t_end && r.see >= t_begin * KT;
-  const bool again = __builtin_amdgcn_readfirstlane(__syncthreads_or(!idle && sees && !in_range(r.l, oacc)));
-  r.m = sees ? kUpRef : -INFINITY;
-  r.l *= kUp;
-  if (again) {
+  auto some_wave = [](bool x) { return __builtin_amdgcn_readfirstlane(__syncthreads_or(x)) != 0; };
+  auto refer = [&](int t_top) {  // to the largest exponents of the tiles up to t_top; the walk begins anew
     float top = -INFINITY;
     offsets(t_begin < n_whole ? KT : p.tokens - t_begin * KT);
-    for (int t = t_begin; t < t_end; ++t) {
+    for (int t = t_begin; t < t_top; ++t) {
       if (t >= n_whole) offsets(p.tokens - t * KT);
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): what was issued before goes to the same place
       __syncthreads();
       issue_k(t, 0);
       fetch_ks(t);
-      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+      __builtin_amdgcn_s_waitcnt(0x0F70);
       __syncthreads();
       ks[0] = kn[0] >> (16 * gg);
       ks[1] = kn[1] >> (16 * gg);
@@ -843,10 +847,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
       top = fmaxf(top, largest(e));
     }
     __syncthreads();
-    r.m = top == -INFINITY ? 0.f : top;
     begin();
-    run(Int<1>());
     r.m = top;
+  };
+  const bool sees = !idle && t_begin < t_end && r.see >= t_begin * KT;
+  bool low = false;  // whether a long walk begins with exponents that do not fit
+  if (t_end - t_begin >= kLong) {
+    refer(t_begin + 1);
+    low = some_wave(sees && r.m > -INFINITY && (r.m < -20.f || r.m > 40.f));
+  }
+  bool again = low;
+  if (!low) {
+    run(Int<0>());
+    again = some_wave(sees && !in_range(r.l, oacc));
+    r.m = sees ? kUpRef : -INFINITY;
+    r.l *= kUp;
+  }
+  for (int t_top = low ? t_begin + 1 : t_end; again; t_top = t_end) {
+    refer(t_top);
+    if (r.m == -INFINITY) r.m = 0.f;
+    run(Int<1>());
+    if (r.l == 0.f) r.m = -INFINITY;
+    again = t_top < t_end && some_wave(sees && !in_range(r.l, oacc));
   }
   if (t_end > t_masked) {
     __syncthreads();

@@ -85,3 +85,32 @@ def test_values_large_and_small(n, hq, hkv, before, exponent, offset):
         _write(V, gen.bf16_bits_to_f32(V) * np.float32(2.0 ** exponent))
         _shift(Q, K, np.full(Q.shape[1], offset))
     _run(n, hq, hkv, before, change)
+
+
+@pytest.mark.parametrize("first,later", [(0.0, 0.0), (-60.0, -60.0), (75.0, 75.0), (0.0, 120.0), (-60.0, 75.0), (-60.0, -250.0)])
+def test_long_walks(first, later):
+    """64 heads, 1024 tokens behind 16500: every workgroup walks over 256 tiles of 64 keys and more.  Scores of the first tile, and of the others, far from 0."""
+    print(f"case attend4 long walk {first} {later}", flush=True)
+    hq, hkv, n, before = 64, 8, 1024, 16500
+
+    def change(Q, K, V):
+        q, k = gen.bf16_bits_to_f32(Q), gen.bf16_bits_to_f32(K)
+        q[..., :32] = 1.5
+        k[..., :32] = later / (32 * 1.5 * 128.0 ** -0.5)  # before it becomes codes: about that far
+        k[:, :64, :32] = first / (32 * 1.5 * 128.0 ** -0.5)
+        _write(Q, q)
+        _write(K, k)
+    ses, c, Q, keys, vals = _setup(hq, hkv, before + n, 5, change)
+    rows, splits = sa.sa_cache4_attend_plan(ses.ctx, n, before)
+    assert (rows, splits) == (128, 1)
+    O = torch.full((hq, n, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    ses.attend(c, dev_bf16(Q[:, before:]), before, O)
+    torch.cuda.synchronize()
+    got = host_f64(O)
+    assert np.isfinite(got).all()
+    for t in (0, 1, 15, 100, 511, 512, 777, 1023):
+        q, k, v = _f64(Q[:, before + t:before + t + 1]), keys[:, :before + t + 1], vals[:, :before + t + 1]
+        want, tol = _reference(q, k, v, before + t, rows)
+        size = np.abs(q) @ np.repeat(np.abs(k), hq // hkv, 0).transpose(0, 2, 1) * 128.0 ** -0.5 * np.log2(np.e)
+        err, tol = np.abs(got[:, t:t + 1] - want), tol + 2.0 ** -20 * np.log(2) * size.max(-1, keepdims=True) * 2 * np.abs(v).max()
+        assert (err <= tol).all(), (t, float((err / tol).max()))
