@@ -307,12 +307,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendOut p) {
   *(bvec *)(p.O + (size_t)(kvh * p.g + row - tok * p.g) * p.o_hs + (size_t)tok * p.o_rs + W * ln) = r;
 }
 
-// all: rows of all KV heads.
-inline void launch_join(const AttendOut &p, int64_t all, hipStream_t st) {
+// all: rows of all KV heads.  one: splits up to which a wave takes a row, 8 or 12.
+inline void launch_join(const AttendOut &p, int64_t all, hipStream_t st, int one = 8) {
+  const unsigned fours = (unsigned)((all + kThreads / 64 - 1) / (kThreads / 64));
   if (p.S > 1) {
     if (p.S > 32) join_kernel<4, 16><<<(unsigned)all, kThreads, 0, st>>>(p);
-    else if (p.S > 8) join_kernel<4, 4><<<(unsigned)all, kThreads, 0, st>>>(p);
-    else join_kernel<1, 8><<<(unsigned)((all + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(p);
+    else if (p.S > one) join_kernel<4, 4><<<(unsigned)all, kThreads, 0, st>>>(p);
+    else if (p.S > 8) join_kernel<1, 12><<<fours, kThreads, 0, st>>>(p);
+    else join_kernel<1, 8><<<fours, kThreads, 0, st>>>(p);
   }
 }
 

@@ -16,7 +16,8 @@ FORMS = [((4, 4), 3, 0, (16, False)), ((8, 2), 61, 333, (16, False)), ((4, 4), 7
          ((64, 1), 130, 0, (32, False)), ((64, 8), 191, 640, (32, False)), ((8, 1), 191, 2000, (32, True)), ((6, 2), 150, 3001, (32, True)),
          ((8, 8), 50, 9000, (32, True)), ((32, 8), 13, 9000, (32, True)), ((40, 1), 47, 4000, (32, True)),
          ((128, 2), 160, 0, (128, False)), ((128, 2), 130, 5, (128, False)), ((128, 2), 100, 70, (128, False)), ((64, 1), 400, 640, (128, False)),
-         ((128, 2), 333, 1000, (128, False)), ((8, 1), 700, 6000, (128, True)), ((64, 1), 47, 9000, (128, True)), ((4, 4), 400, 20000, (128, True))]
+         ((128, 2), 333, 1000, (128, False)), ((8, 1), 700, 6000, (128, True)), ((64, 1), 47, 9000, (128, True)), ((4, 4), 400, 20000, (128, True)),
+         ((32, 8), 90, 8000, (128, True))]
 
 
 def _made(heads, n, before, form, seed, change=None):
