@@ -587,14 +587,15 @@ class Session:
         n = K.shape[1]
         shape = (self._hkv, n, 128)
         call = self._lib.sa_cache4_append if cache.block is None else self._lib.sa_cache_append
-        st = call(self.ctx, struct, _rows(K, shape, self._bf16, device, "K"), _rows(V, shape, self._bf16, device, "V"),
-                                       n, pos, self._raw_stream(device))
+        st = call(self.ctx, struct, _rows(K, shape, self._bf16, device, "K"), _rows(V, shape, self._bf16, device, "V"), n, pos,
+                  self._raw_stream(device))
         if st:
             _check(st, self.ctx)
 
     def read(self, cache, K, V, pos=0, tokens=None):
         """Tokens pos, pos + 1, ... of a cache into K, V [n_kv_heads, n, 128] (either may be None).  tokens: how many the cache holds,
-        pos + n if it is left out (a 4-bit cache is read the same for any)."""
+        pos + n if it is left out, as in attend().  An 8-bit cache that holds more needs it, since it says which tokens stand in
+        full blocks and which are open; a 4-bit cache is read the same for any."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
@@ -651,7 +652,7 @@ class Session:
         q = _rows(Q, shape, self._bf16, device, "Q")
         call = self._lib.sa_cache4_attend if cache.block is None else self._lib.sa_cache_attend
         st = call(self.ctx, struct, q, n, pos, q if O is Q else _rows(O, shape, self._bf16, device, "O"), scratch, size,
-                                       self._raw_stream(device))
+                  self._raw_stream(device))
         if st:
             _check(st, self.ctx)
 
