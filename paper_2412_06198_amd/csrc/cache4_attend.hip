@@ -355,6 +355,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
   r.l *= kUp;
   if (again) {  // this wave's keys
     float top = -INFINITY;
+    auto whole_tiles = [&] {  // after the last tile changed the rows to read
+      k_row = q;
+      v_row[0] = (unsigned)lane >> 2;
+      v_row[1] = ((unsigned)lane >> 2) + 16;
+    };
+    whole_tiles();
     for (int t = t_first; t < t_end; t += WK) {
       fetch(t);
       const uint32_t ksw = ks >> (16 * gg);
@@ -366,9 +372,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
       top = fmaxf(top, largest(e));
     }
     r.m = top == -INFINITY ? 0.f : top;
-    k_row = q;  // the walk's last tile changed them
-    v_row[0] = (unsigned)lane >> 2;
-    v_row[1] = ((unsigned)lane >> 2) + 16;
+    whole_tiles();
     fetch(t_first);
     run(Int<1>());
     r.m = top;

@@ -114,3 +114,19 @@ def test_long_walks(first, later):
         size = np.abs(q) @ np.repeat(np.abs(k), hq // hkv, 0).transpose(0, 2, 1) * 128.0 ** -0.5 * np.log2(np.e)
         err, tol = np.abs(got[:, t:t + 1] - want), tol + 2.0 ** -20 * np.log(2) * size.max(-1, keepdims=True) * 2 * np.abs(v).max()
         assert (err <= tol).all(), (t, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("n,hq,hkv,before,far", [(130, 64, 1, 0, 10), (130, 64, 1, 0, 31), (191, 64, 8, 642, 30), (150, 6, 2, 3007, 2950)])
+def test_a_far_key_of_a_wave_that_ends_inside_a_tile(n, hq, hkv, before, far):
+    """32 rows a workgroup: the wave that ends with the last, partial tile takes its whole tiles with all their keys when it starts anew."""
+    print(f"case attend4 far key {n} {hq} {hkv} {before} {far}", flush=True)
+
+    def change(Q, K, V):
+        q, k = gen.bf16_bits_to_f32(Q), gen.bf16_bits_to_f32(K)
+        q[..., :32], k[..., :32] = 1.5, 0.0
+        k[:, far, :32] = 200.0 / (32 * 1.5 * 128.0 ** -0.5)
+        _write(Q, q)
+        _write(K, k)
+    ses = sa.Session(hq, hkv, 256, 64, 32, keep=0.5)
+    assert sa.sa_cache4_attend_plan(ses.ctx, n, before)[0] == 32
+    _run(n, hq, hkv, before, change)
