@@ -116,9 +116,11 @@ def test_long_walks(first, later):
         assert (err <= tol).all(), (t, float((err / tol).max()))
 
 
-@pytest.mark.parametrize("n,hq,hkv,before,far", [(130, 64, 1, 0, 10), (130, 64, 1, 0, 31), (191, 64, 8, 642, 30), (150, 6, 2, 3007, 2950)])
-def test_a_far_key_of_a_wave_that_ends_inside_a_tile(n, hq, hkv, before, far):
-    """32 rows a workgroup: the wave that ends with the last, partial tile takes its whole tiles with all their keys when it starts anew."""
+@pytest.mark.parametrize("rows,n,hq,hkv,before,far", [(32, 130, 64, 1, 0, 10), (32, 130, 64, 1, 0, 31), (32, 191, 64, 8, 642, 30), (32, 150, 6, 2, 3007, 2950),
+                                                      (128, 160, 128, 2, 0, 10), (128, 130, 128, 2, 5, 63), (128, 333, 128, 2, 1000, 1020),
+                                                      (128, 90, 32, 8, 8000, 7990), (16, 61, 8, 2, 337, 250), (16, 12, 16, 2, 3001, 2999)])
+def test_a_far_key_of_a_wave_that_ends_inside_a_tile(rows, n, hq, hkv, before, far):
+    """The wave that ends with the last, partial tile takes its whole tiles with all their keys when it starts anew."""
     print(f"case attend4 far key {n} {hq} {hkv} {before} {far}", flush=True)
 
     def change(Q, K, V):
@@ -128,5 +130,5 @@ def test_a_far_key_of_a_wave_that_ends_inside_a_tile(n, hq, hkv, before, far):
         _write(Q, q)
         _write(K, k)
     ses = sa.Session(hq, hkv, 256, 64, 32, keep=0.5)
-    assert sa.sa_cache4_attend_plan(ses.ctx, n, before)[0] == 32
+    assert sa.sa_cache4_attend_plan(ses.ctx, n, before)[0] == rows
     _run(n, hq, hkv, before, change)

@@ -10,6 +10,7 @@ import paper_2412_06198_amd as sa
 from oracle import cache4 as oc
 from oracle import oracle as orc
 from gpu_util import host_f64, upload_index
+from test_gpu_cache4_attend import _reference
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +119,25 @@ def test_read_of_8_bits_past_32_bits():
     ses.read(c, x, None, cap - 320)
     ses.read(near, y, None, 0)
     assert torch.equal(x, y)
+
+
+def test_more_row_tiles_than_a_grid_is_deep():
+    """128 heads on 2 KV heads, 66000 tokens at once: 33000 tiles of 128 query rows a KV head, over the 32768 that stand one behind the other."""
+    print("case attend4 33000 row tiles", flush=True)
+    hq, hkv, n = 128, 2, 66000
+    ses = sa.Session(hq, hkv, 256, 64, 32, keep=0.5)
+    c = ses.cache4(n)
+    made = torch.Generator(device="cuda").manual_seed(3)
+    K, V = (torch.randn((hkv, n, 128), generator=made, device="cuda").bfloat16() for _ in range(2))
+    ses.append(c, K, V, 0)
+    ses.read(c, K, V)
+    Q = torch.randn((hq, n, 128), generator=made, device="cuda", dtype=torch.bfloat16)
+    assert sa.sa_cache4_attend_plan(ses.ctx, n, 0) == (128, 1)
+    O = torch.full_like(Q, 7.0)
+    ses.attend(c, Q, 0, O)
+    torch.cuda.synchronize()
+    assert not bool((O == 7.0).all(-1).any())
+    for t in (0, 1, 2, 447, 448, 449, 33000, 65535, 65536, 65999):  # 2 tokens a tile: the first 232 tiles stand beside the KV heads
+        want, tol = _reference(host_f64(Q[:, t:t + 1]), host_f64(K[:, :t + 1]), host_f64(V[:, :t + 1]), t, 128)
+        err = np.abs(host_f64(O[:, t:t + 1]) - want)
+        assert (err <= tol).all(), (t, float((err / tol).max()))
