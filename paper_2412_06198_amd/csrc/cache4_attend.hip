@@ -171,6 +171,20 @@ __device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
     for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
   return l > 0x1p-40f && l < 0x1p80f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f;
 }
+// A row's sums hold by themselves, up to the ends of fp32, but they are joined with those of four waves and of up to 256 splits, which may be done once more,
+// with other references: the power of two of l goes into the reference, so that l is in [0.5, 1) and an output at most as large as the largest of V.
+// Then sums of parts stay far from the ends, and exp2(m - M), which is 0 below 2^-126, is what a part weighs.  l is between 2^-40 and 2^121, so that 2^-x
+// is a normal number; 0 (no key), infinite or NaN it stays as it is.  m + x is rounded where m is no whole number, by no more than the scores were.
+__device__ inline void settle(float &m, float &l, f32x16 (&o)[4]) {
+  const int x = __builtin_amdgcn_frexp_expf(l);
+  const float s = __builtin_ldexpf(1.f, -x);
+  m += (float)x;
+  l *= s;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] *= s;
+}
 // The groups of V that are NaN among the keys first .. first + 63 (rowbad: a byte for each, a bit for each group; 0 from key `end` on), for a row
 // that sees keys up to `see`.
 __device__ inline void put_nan(const uint8_t *rowbad, int first, int end, int see, f32x16 (&o)[4]) {
@@ -384,6 +398,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
       put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
     }
   }
+  settle(r.m, r.l, oacc);
   put_waves(p, kvh, r0, sp, r.m, r.l, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
@@ -878,6 +893,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
   }
+  settle(r.m, r.l, oacc);
   if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.m, r.l, oacc);
 }
 
