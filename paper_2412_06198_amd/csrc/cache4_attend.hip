@@ -171,12 +171,13 @@ __device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
     for (int db = 0; db < 4; ++db) odd[db] = __builtin_fmaf(oacc[db][k], 0.f, odd[db]);
   return l > 0x1p-40f && l < 0x1p80f && odd[0] + odd[1] + odd[2] + odd[3] == 0.f;
 }
-// A row's sums hold by themselves, up to the ends of fp32, but they are joined with those of four waves and of up to 256 splits, which may be done once more,
-// with other references: the power of two of l goes into the reference, so that l is in [0.5, 1) and an output at most as large as the largest of V.
-// Then sums of parts stay far from the ends, and exp2(m - M), which is 0 below 2^-126, is what a part weighs.  l is between 2^-40 and 2^121, so that 2^-x
-// is a normal number; 0 (no key), infinite or NaN it stays as it is.  m + x is rounded where m is no whole number, by no more than the scores were.
-__device__ inline void settle(float &m, float &l, f32x16 (&o)[4]) {
-  const int x = __builtin_amdgcn_frexp_expf(l);
+// A row's sums over `keys` keys hold by themselves, up to the ends of fp32, but they are joined with those of four waves and of up to 256 splits, some of which
+// may have been done once more.  So where their mean probability is above 1, its power of two goes into the reference, which is then at most about the largest
+// exponent: l is below 2 keys, an output at most that times the largest of V, and a part whose exp2(m - M) is 0, below 2^-126, weighs less than 2^-125 keys.
+// l is below 2^121, so that 2^-x is a normal number; 0 (no key), infinite or NaN it stays so.  m + x is rounded where m is no whole
+// number, by no more than the scores were.
+__device__ inline void settle(float &m, float &l, f32x16 (&o)[4], int keys) {
+  const int x = max(__builtin_amdgcn_frexp_expf(l) - (32 - __builtin_clz((uint32_t)max(keys, 1))), 0);
   const float s = __builtin_ldexpf(1.f, -x);
   m += (float)x;
   l *= s;
@@ -390,6 +391,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
     fetch(t_first);
     run(Int<1>());
     r.m = top;
+  } else {
+    settle(r.m, r.l, oacc, (t_end - t_first + WK - 1) / WK * KT);
   }
   if (t_end > t_masked) {
     __syncthreads();
@@ -398,7 +401,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
       put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
     }
   }
-  settle(r.m, r.l, oacc);
   put_waves(p, kvh, r0, sp, r.m, r.l, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
@@ -882,7 +884,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     r.m = sees ? kUpRef : -INFINITY;
     r.l *= kUp;
   }
+  bool largest_off = false;  // whether it is the largest exponents of all keys that were subtracted
   for (int t_top = low ? t_begin + 1 : t_end; again; t_top = t_end) {
+    largest_off = t_top == t_end;
     refer(t_top);
     if (r.m == -INFINITY) r.m = 0.f;
     run(Int<1>());
@@ -893,7 +897,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
   }
-  settle(r.m, r.l, oacc);
+  if (!largest_off) settle(r.m, r.l, oacc, (t_end - t_begin) * KT);
   if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.m, r.l, oacc);
 }
 
