@@ -281,6 +281,8 @@ def _cache(cache):
 
 def sa_cache_append(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
     _check(library().sa_cache_append(ctx, _cache(cache), K, V, n, pos, stream), ctx)
+    if isinstance(cache, Cache):
+        cache.tokens = pos + n
 
 
 def sa_cache_decode(ctx, cache, q, index: SaIndex, pos, o, stream=None):
@@ -317,6 +319,8 @@ def sa_cache4_bytes(ctx, capacity):
 
 def sa_cache4_append(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
     _check(library().sa_cache4_append(ctx, _cache(cache), K, V, n, pos, stream), ctx)
+    if isinstance(cache, Cache4):
+        cache.tokens = pos + n
 
 
 def sa_cache4_read(ctx, cache, K: SaRows, V: SaRows, n, pos, stream=None):
@@ -368,7 +372,10 @@ _ROTARY_FIELDS = {name for name, _ in SaRotaryConfig._fields_}
 
 class Cache:
     """The six buffers of an 8-bit key/value cache (see sa_cache in include/sa.h): k, v uint8 [n_kv_heads, capacity, 128],
-    k_scale, v_scale fp32 [n_kv_heads, capacity / block], k_open, v_open bf16 [n_kv_heads, block, 128], contiguous."""
+    k_scale, v_scale fp32 [n_kv_heads, capacity / block], k_open, v_open bf16 [n_kv_heads, block, 128], contiguous.
+    tokens: how many it holds, which every append() on this object sets; None where no call has said so."""
+
+    tokens = None
 
     def __init__(self, k, v, k_scale, v_scale, k_open, v_open, cache_type=SA_CACHE_E4M3):
         if k.ndim != 3 or k_open.ndim != 3 or k_open.shape[1] == 0:
@@ -392,7 +399,9 @@ class Cache:
 
 class Cache4:
     """The four buffers of a 4-bit key/value cache (see sa_cache4 in include/sa.h): k, v uint8 [n_kv_heads, capacity, 64],
-    k_scale, v_scale uint8 [n_kv_heads, capacity, 4], contiguous."""
+    k_scale, v_scale uint8 [n_kv_heads, capacity, 4], contiguous.  tokens: as of Cache."""
+
+    tokens = None
 
     def __init__(self, k, v, k_scale, v_scale):
         if k.ndim != 3 or k.shape[2] != 64:
@@ -560,14 +569,18 @@ class Session:
         kinds = [((h, capacity, 128), t.uint8)] * 2 + [((h, capacity // b), t.float32)] * 2 + [((h, b, 128), t.bfloat16)] * 2
         bufs = [t.empty(shape, dtype=kind, device=self.ws.device) for shape, kind in kinds]  # self.device may have no index
         assert [x.nbytes for x in bufs] == sizes
-        return Cache(*bufs, cache_type)
+        made = Cache(*bufs, cache_type)
+        made.tokens = 0
+        return made
 
     def cache4(self, capacity):
         """An empty 4-bit cache for `capacity` tokens, for the same calls as cache()."""
         sizes = sa_cache4_bytes(self.ctx, capacity)
         bufs = [self.torch.empty((self.cfg.n_kv_heads, capacity, last), dtype=self.torch.uint8, device=self.ws.device) for last in (64, 64, 4, 4)]
         assert [x.nbytes for x in bufs] == sizes
-        return Cache4(*bufs)
+        made = Cache4(*bufs)
+        made.tokens = 0
+        return made
 
     def _own(self, cache):
         """The cache's struct, if the cache fits the session; a 4-bit cache has no blocks."""
@@ -578,8 +591,9 @@ class Session:
 
     def append(self, cache, K, V, pos):
         """K, V [n_kv_heads, n, 128] behind the pos tokens that the cache holds.  To take tokens back across a block that a call
-        has filled: copies of cache.k_open and cache.v_open from before it, put back, and append() again from its pos on; a 4-bit
-        cache has no blocks, append() from any pos on."""
+        has filled: copies of cache.k_open and cache.v_open from before it, put back, and append() again from its pos on, of no tokens
+        if none stay; a 4-bit cache has no blocks, append() from any pos on.  cache.tokens is pos + n then (in a capture, too: a
+        replay behind other calls does not set it again)."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
@@ -591,11 +605,13 @@ class Session:
                   self._raw_stream(device))
         if st:
             _check(st, self.ctx)
+        cache.tokens = pos + n
 
     def read(self, cache, K, V, pos=0, tokens=None):
         """Tokens pos, pos + 1, ... of a cache into K, V [n_kv_heads, n, 128] (either may be None).  tokens: how many the cache holds,
-        pos + n if it is left out, as in attend().  An 8-bit cache that holds more needs it, since it says which tokens stand in
-        full blocks and which are open; a 4-bit cache is read the same for any."""
+        which says what stands in full blocks of an 8-bit cache and what is open; cache.tokens if it is left out, but no fewer than
+        pos + n.  A cache around buffers that were filled elsewhere has no cache.tokens: a part that is not its end needs the
+        number.  A 4-bit cache is read the same for any."""
         device, struct = self._gpu, self._own(cache)
         if self._get_device() != device:
             with self.torch.cuda.device(device):
@@ -606,7 +622,7 @@ class Session:
         shape, bf16 = (self._hkv, n, 128), self._bf16
         k = _NO_ROWS if K is None else _rows(K, shape, bf16, device, "K")
         v = _NO_ROWS if V is None else _rows(V, shape, bf16, device, "V")
-        held = pos + n if tokens is None else tokens
+        held = max(pos + n, cache.tokens or 0) if tokens is None else tokens
         if held < pos + n:
             raise SaError(1, f"the cache holds {held} tokens, not {pos + n}")
         if cache.block is None:
