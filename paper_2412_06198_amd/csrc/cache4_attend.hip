@@ -175,7 +175,8 @@ __device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
 // may have been done once more.  So where their mean probability is above 1, its power of two goes into the reference, which is then at most about the largest
 // exponent: l is below 2 keys, an output at most that times the largest of V, and a part whose exp2(m - M) is 0, below 2^-126, weighs less than 2^-125 keys.
 // l is below 2^121, so that 2^-x is a normal number; 0 (no key), infinite or NaN it stays so.  m + x is rounded where m is no whole
-// number, by no more than the scores were.
+// number, by no more than the scores were.  kLargestOff: the largest exponents of all keys were subtracted, so that there is nothing to move.
+constexpr int kLargestOff = 0x7FFFFFFF;
 __device__ inline void settle(float &m, float &l, f32x16 (&o)[4], int keys) {
   const int x = max(__builtin_amdgcn_frexp_expf(l) - (32 - __builtin_clz((uint32_t)max(keys, 1))), 0);
   const float s = __builtin_ldexpf(1.f, -x);
@@ -391,8 +392,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
     fetch(t_first);
     run(Int<1>());
     r.m = top;
-  } else {
-    settle(r.m, r.l, oacc, (t_end - t_first + WK - 1) / WK * KT);
   }
   if (t_end > t_masked) {
     __syncthreads();
@@ -401,6 +400,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
       put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
     }
   }
+  // Here, not beside the pass above: there the compiler spills the outputs, and a pass that is done once more takes ten times as long.
+  settle(r.m, r.l, oacc, again ? kLargestOff : (t_end - t_first + WK - 1) / WK * KT);
   put_waves(p, kvh, r0, sp, r.m, r.l, oacc, &lds.o[0][0][0], s_m, s_l);
 }
 
@@ -884,9 +885,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     r.m = sees ? kUpRef : -INFINITY;
     r.l *= kUp;
   }
-  bool largest_off = false;  // whether it is the largest exponents of all keys that were subtracted
+  int keys = (t_end - t_begin) * KT;
   for (int t_top = low ? t_begin + 1 : t_end; again; t_top = t_end) {
-    largest_off = t_top == t_end;
+    if (t_top == t_end) keys = kLargestOff;
     refer(t_top);
     if (r.m == -INFINITY) r.m = 0.f;
     run(Int<1>());
@@ -897,7 +898,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_rows_kernel(Attend4Args p
     __syncthreads();
     for (int t = max(t_begin, t_masked); t < t_end; ++t) put_nan(rowbad + (t - t_masked) * KT, t * KT, (t + 1) * KT, r.see, oacc);
   }
-  if (!largest_off) settle(r.m, r.l, oacc, (t_end - t_begin) * KT);
+  settle(r.m, r.l, oacc, keys);
   if (r0 + 32 * wave + q < p.rows) put_row(p, kvh, r.row, head, tok, sp, gg, r.m, r.l, oacc);
 }
 
