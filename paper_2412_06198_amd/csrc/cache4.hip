@@ -7,7 +7,7 @@
 // Both directions read and write everything once: the bound is HBM.  A row is taken by 16 lanes, 8 elements each, so that every access of
 // a wave is contiguous (16 bytes a lane in bf16, 4 in codes); a group is four lanes, whose largest magnitude is two lane moves.  128K tokens of 8 heads, 680 MB: 110 us
 // to append, 109 to read back (6.2 TB/s; a device copy moves 5.1), 128 to read back from 8 bits (6.3 TB/s).  What is read back goes past the caches
-// (120 us with ordinary stores), the codes do not, since they are read next (10K tokens stored and read back 19.5 us, 21.0 past them).
+// (120 us with ordinary stores), the codes do not, since they are read next (10K tokens stored and read back 18.8 to 19.6 us, 21.0 past them).
 #include "cache4_codes.h"
 #include "cache_codes.h"
 #include "sa_internal.h"

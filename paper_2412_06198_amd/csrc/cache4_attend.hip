@@ -161,7 +161,8 @@ __device__ inline float largest(const f32x16 (&e)[HF]) {
 // enough (a row's sum beyond 2^80 or below 2^-40, or an output that is no number, of V beyond 2^85 or NaN) the rows are done once more, with
 // their largest exponents subtracted and V as it is.  With 128 rows a long walk looks at its first tile ahead, and where that is far from 0
 // already, subtracts the largest exponents of this tile from the start (2048 tokens of 32 heads at 64K keys, all scores 40 lower: 4000 us without
-// the look, 1580 with it; as they come 1555).
+// the look, 1555 with it; as they come 1510).  Shorter walks, and all with 32 rows, pay for the second pass: scores 40 lower or 60 higher, 200 tokens at 8000 keys
+// 40 -> 71 us, 2048 at 8000 220 -> 545; 32 rows, 500 tokens at 500 keys 13.4 -> 23.4, 50 at 5000 16.5 -> 28.
 constexpr float kUp = 0x1p40f, kUpRef = -40.f;
 __device__ inline bool in_range(float l, const f32x16 (&oacc)[4]) {
   float odd[4] = {};  // 0, or NaN where an output is no number
@@ -217,7 +218,7 @@ __device__ inline float sum_blocks(float x) {
 
 // 32 query rows a workgroup, every wave its own keys, tiles of 32 of them; no barriers on the way.  A lane reads the half row of K that it multiplies
 // itself, so that only V goes through LDS, between the products of K.  Bound: one tile after the other, which two waves a SIMD half hide:
-// products, their exponentials, V's way through LDS.  500 tokens of 32 heads at 1000 keys 16.7 us, 50 at 5000 16.4 with the join (8 bits: 19.7 at 500).
+// products, their exponentials, V's way through LDS.  500 tokens of 32 heads at 1000 keys 17 us, 50 at 5000 16.5 with the join (8 bits: 19.7 at 500).
 template <int PARTS>
 __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p) {
   constexpr int KT = 32, WK = kThreads / 64;  // keys per tile, waves
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend4_few_kernel(Attend4Args p)
 // Steps: 16 query rows a workgroup, every wave its own keys, tiles of 32 of them.  One v_mfma_scale_f32_16x16x128 takes 16 keys, whole rows of K: a
 // lane reads one group of a key and multiplies it with the same group of its query row (lane & 15).  Half the products, exponentials and registers of 32
 // rows, so that four waves a SIMD, instead of two, have reads on their way.  Bound: HBM on long caches, one token of 32 heads at 128K keys reads 143 MB in
-// 28.0 us (5.1 TB/s), 32.3 with the join (32 rows a workgroup: 39.6); the chain of reads on short ones, 5 tokens of 8 heads on one KV head at 10K keys 9.1.
+// 28.0 us (5.1 TB/s), 32.3 to 33.1 with the join (32 rows a workgroup: 39.6); the chain of reads on short ones, 5 tokens of 8 heads on one KV head at 10K keys 9.1.
 __global__ __launch_bounds__(kThreads, 4) void attend4_step_kernel(Attend4Args p) {
   constexpr int KT = 32, WK = kThreads / 64, ROWS = kRowsStep;
   constexpr int kMasked = 2;  // tiles that some rows see and others do not, at most: 15 keys
@@ -907,8 +908,8 @@ size_t max_slots(const Shape &sh) { return (size_t)sh.n_cu * 256; }
 
 // Which kernel, and into how many splits the keys go: the least of an estimate over the three kernels and over splits that fill a quarter of the card, a
 // half, .. all that a compute unit holds at once.  The terms were fitted (us) to some 13000 measurements of 1500 drawn shapes of 4 to 64
-// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these the choice is 0.5 % slower than the best of all kernels and splits in the
-// mean, and 22 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
+// heads, 1 to 2048 tokens and up to 131072 keys, in recorded loops; over these, the 1100 that the terms were fitted to among them, the choice is 0.5 % slower than the
+// best of all kernels and splits in the mean, and 21.5 % at worst.  There is no term for the rate of memory or the power limit, so that for the longest calls it is less than the time.
 //                                              16 rows   32 rows, up to 64 in all   32 rows   128 rows
 //   start and end                              3.45      5.65                       5.65      5.2
 //   keys of a round of a workgroup's waves     128       128                        128       64
@@ -985,7 +986,8 @@ hipError_t launch_cache4_attend(const Shape &sh, const sa_cache4 &c, sa_rows Q, 
   else if (plan.rows == kRowsFew && a.rows <= 2 * kRowsFew) attend4_few_kernel<2><<<grid, kThreads, 0, st>>>(a);
   else if (plan.rows == kRowsFew) attend4_few_kernel<1><<<grid, kThreads, 0, st>>>(a);
   else attend4_rows_kernel<<<grid, kThreads, 0, st>>>(a);
-  // many rows of 9 to 12 splits: a wave a row (200 tokens of 32 heads at 8000 keys, 9 splits: 42.0 -> 40.6 us; 4 tokens, 12 splits: 9.2 -> 9.5)
+  // Many rows of 9 to 12 splits: a wave a row, against four of them (us, whole calls, 33 shapes): up to 400 rows 0 to 0.3 slower (64 rows, 12 splits 7.6 instead of 7.3), at 768
+  // the same (14.7, 14.8), from 2500 on 0.5 to 1.6 faster (5120 rows, 12 splits 42.6 instead of 43.2; 6400, 9 splits 49.2 instead of 50.9).
   launch_join(a, all, st, all >= 1024 ? 12 : 8);
   return hipGetLastError();
 }

@@ -1,8 +1,8 @@
 // One decode step over the prefill index, K and V out of the 4-bit cache: the keys, their order and the launch are those of the step
 // over the 8-bit cache (cache_decode.hip), half the bytes.  A key is read by 16 lanes as 64 bytes of codes of K and of V, and the two bytes of
 // their group's scales, which the conversion to fp32 applies.  There is no open block, so all keys are rows of one kind.  The bound is a launch and the
-// round trips to memory that follow one another, as there: 8 heads at 4K tokens 7.0 us with the host's call, 32 heads at 128K tokens, 3 % kept,
-// 11.1.
+// round trips to memory that follow one another, as there: 8 heads at 4K tokens 6.6 to 6.9 us with the host's call, 32 heads at 128K tokens, 3 %
+// kept, 11.0 to 11.1.
 #include <algorithm>
 
 #include "cache4_codes.h"
